@@ -60,6 +60,7 @@ extern "C" {
 #endif
 
 #define LRBI_MAX_RANK 256
+#define LRBI_MAX_TOP 64 /* most likely words that lrbi_token_logprobs gives per token */
 
 typedef struct lrbi_desc {
     int64_t m, n;   /* rows and columns of W                                   */
@@ -445,6 +446,93 @@ int lrbi_nmf_workspace_bytes(const lrbi_desc *desc, uint64_t *bytes);
 int lrbi_nmf(const lrbi_desc *desc, lrbi_dtype dtype, const void *dW, int64_t ldw, int32_t method,
              float w_threshold, float amplify, float *dMp, float *dMz, int32_t iters, float eps,
              void *dWorkspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Pruned weights in 4 bits (OCP microscaling, MXFP4): blocks of 32 neighbouring weights of a row, each a 4-bit floating-point
+ * code (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) times the block's scale 2^(b - 127), b one byte.
+ *   codes   m rows of ldc bytes (a multiple of 16, >= 16 * ceil(n / 32)), 16-byte aligned; column j of a row is the lower
+ *           (j even) or upper half of byte j / 2; a last block that n cuts off is filled up with zero codes.
+ *   scales  m rows of lds bytes (a multiple of 4, >= ceil(n / 32)), 4-byte aligned.  255 makes a block NaN.
+ *
+ * lrbi_quant_pack: W (m x n row-major of `dtype`, ldw >= n) into codes and scales.  The mask (Eq. 3) is applied here: a pruned
+ *   weight becomes code 0, whatever value is stored under it, and does not count for the scale.  dIp_packed and dIz_packed
+ *   both NULL: nothing is pruned.  A block's scale is the smallest power of two at which its largest magnitude does not round
+ *   past 6 (not below 2^-125 or above 2^125, f16: 2^-23 and 2^13, so that every code's value is a number of the type; larger
+ *   weights become the largest code); a weight is rounded to the nearest code, ties to the even one.  A block that keeps an
+ *   infinity or a NaN gets scale 255.  Bytes past the last block of a row are left as they are.  One kernel launch.
+ * lrbi_quant_unpack: the values, as m x n numbers of `dtype`; exact at every scale that lrbi_quant_pack writes for this type,
+ *   otherwise rounded to it.  One kernel launch.
+ * lrbi_quant_matvec: Y = Wq X with the values Wq of codes and scales, X n x N and Y m x N row-major of `dtype` (ldx, ldy >= N;
+ *   Y is overwritten).  f16 / bf16: products exact, fp32 sums; f32: X is taken as three bf16 parts whose products are exact.
+ *   The order of the sums is fixed (identical bits from call to call); one rounding to nearest-even on store.  Values that are
+ *   no numbers of `dtype` (codes packed from another type) are rounded to it first.  X should be finite: an infinity times a
+ *   zero code is NaN.  Any N; made for one to a few dozen columns (16, or 5 in f32, take the time of one).  For larger
+ *   batches lrbi_quant_unpack and lrbi_masked_gemm are the way.  One kernel launch.
+ * Errors: those of the argument checks above; m, n, N not positive or beyond 2^31 - 256 are LRBI_ERR_SHAPE; one of the two
+ * factors without the other LRBI_ERR_NULL.
+ */
+int lrbi_quant_pack(const lrbi_desc *desc, lrbi_dtype dtype, const void *dW, int64_t ldw, const void *dIp_packed,
+                    const void *dIz_packed, void *dCodes, int64_t ldc, void *dScales, int64_t lds, void *stream);
+int lrbi_quant_unpack(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m,
+                      int64_t n, void *dW, int64_t ldw, void *stream);
+int lrbi_quant_matvec(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m,
+                      int64_t n, const void *dX, int64_t ldx, int64_t N, void *dY, int64_t ldy, void *stream);
+
+/*
+ * Activation checkpoints in 8 bits (OCP microscaling, MXFP8 E4M3): a layer's input X (n x N row-major, the X of
+ * lrbi_masked_gemm) kept for the backward pass as blocks of 32 neighbouring batch columns of a row, each value an 8-bit code
+ * (sign, 4 exponent bits, 3 mantissa bits: up to 448, multiples of 2^-9 at the lower end, 0x7F and 0xFF NaN) times the block's
+ * scale 2^(b - 127).  1.03 bytes a value.
+ *   codes   n rows of ldc bytes (a multiple of 16, >= 32 * ceil(N / 32)), 16-byte aligned; a last block that N cuts off is
+ *           filled up with zeros.      scales  n rows of lds bytes (a multiple of 4, >= ceil(N / 32)), 4-byte aligned.
+ *
+ * lrbi_checkpoint_pack: the scale is the smallest power of two at which the block's largest finite magnitude does not round
+ *   past 448 (within 2^-117 .. 2^120, f16: 2^-15 .. 2^8); a value is rounded to the nearest code, ties to the even one: off by
+ *   at most 2^-4 of itself, or 2^-10 scales.  Magnitudes beyond 1.875 * 2^127 (f16: 61440) are cut to that.  Infinities and NaN
+ *   become NaN, alone.  Bytes past the last block of a row are left as they are.  One kernel launch.
+ * lrbi_checkpoint_unpack: the values as numbers of `dtype`, exact for the type they came from.  One kernel launch.
+ * lrbi_checkpoint_grad: lrbi_masked_grad with X the checkpoint's values: dW = (dY Xq^T) o I_a, the gradient with respect to
+ *   W, read in 8 bits and widened exactly inside the kernel.  Arguments, masking, accumulation and rounding as there.  One
+ *   kernel launch.
+ * Errors: those of the argument checks above; sizes not positive or beyond 2^31 - 256 are LRBI_ERR_SHAPE.
+ */
+int lrbi_checkpoint_pack(lrbi_dtype dtype, const void *dX, int64_t ldx, int64_t n, int64_t N, void *dCodes, int64_t ldc,
+                         void *dScales, int64_t lds, void *stream);
+int lrbi_checkpoint_unpack(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t n,
+                           int64_t N, void *dX, int64_t ldx, void *stream);
+int lrbi_checkpoint_grad(const lrbi_desc *desc, lrbi_dtype dtype, const void *dDY, int64_t lddy, const void *dCodes,
+                         int64_t ldc, const void *dScales, int64_t lds, int64_t N, const void *dIp_packed,
+                         const void *dIz_packed, void *dDW, int64_t lddw, void *stream);
+
+/*
+ * Token log probabilities of a language model.  The logits are the Y of a masked product: V x N row-major of `dtype`,
+ * ldl >= N, row v = word v, column q = token q.  With p = softmax of column q:
+ *   dLogp[q]     log p of word dTok[q].  A negative word stands for padding: 0.  A word >= V: NaN.  dTok and dLogp: both or neither.
+ *   dEntropy[q]  - sum_v p_v log p_v.  May be NULL.
+ *   dStats       [2][N]: the largest logit, and the base-2 logarithm of sum_v e^(x_v - largest); the logarithm of the sum of
+ *                exponentials is dStats[q] + ln 2 * dStats[N + q].  lrbi_token_logprobs_grad takes it.
+ *   dTopIds, dTopLogp  [top][N]: the `top` most likely words (0 <= top <= LRBI_MAX_TOP; both unused at 0), the most likely
+ *                first, equal logits by the lower word, and their log p.  A word of logit -infinity or NaN is none: where
+ *                fewer are left the rest is word -1 at -infinity.
+ *   Logits of -infinity (words a token may not use) have probability 0.  A column of nothing else: entropy 0, log p and largest
+ *   logit -infinity, no top words.  A column that holds a NaN or +infinity: NaN log p and entropy (top words: by their logits).
+ *   dWorkspace: required, 16-byte aligned, at least lrbi_token_logprobs_workspace_bytes bytes (LRBI_ERR_WORKSPACE
+ *   otherwise).  fp32 arithmetic in a fixed order (identical bits from call to call).  Two kernel launches.
+ *
+ * lrbi_token_logprobs_grad: the gradient of sum_q (dGLogp[q] dLogp[q] + dGEntropy[q] dEntropy[q]) with respect to the logits:
+ *   dDL[v][q] = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy), V x N of `dtype`, lddl >= N.  It is the dY of
+ *   lrbi_masked_gemm_t, lrbi_masked_grad and lrbi_checkpoint_grad.  dStats, dEntropy: as the forward call left them.  dGLogp (with dTok) or dGEntropy
+ *   (with dEntropy) may be NULL, not both.  A padded token takes no gl; a column whose gl and gh are 0 gets zeros whatever
+ *   its logits.  A word >= V: NaN.  dDL may be dL itself with lddl = ldl (not otherwise overlap it).  One kernel launch.
+ * Errors: sizes not positive or beyond 2^31 - 256, top out of range: LRBI_ERR_SHAPE; ldl, lddl < N: LRBI_ERR_PITCH.
+ */
+int lrbi_token_logprobs_workspace_bytes(lrbi_dtype dtype, int64_t V, int64_t N, int32_t top, uint64_t *bytes);
+int lrbi_token_logprobs(lrbi_dtype dtype, const void *dL, int64_t ldl, int64_t V, int64_t N, const int64_t *dTok,
+                        float *dLogp, float *dEntropy, float *dStats, int32_t top, int64_t *dTopIds, float *dTopLogp,
+                        void *dWorkspace, uint64_t workspace_bytes, void *stream);
+int lrbi_token_logprobs_grad(lrbi_dtype dtype, const void *dL, int64_t ldl, int64_t V, int64_t N, const int64_t *dTok,
+                             const float *dStats, const float *dEntropy, const float *dGLogp, const float *dGEntropy,
+                             void *dDL, int64_t lddl, void *stream);
 
 #ifdef __cplusplus
 }

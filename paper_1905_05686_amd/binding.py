@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from collections import namedtuple
 
 import numpy as np
 
@@ -95,7 +96,18 @@ def load_library():
     lib.lrbi_nmf.argtypes = [pd, ctypes.c_int, vp, i64, i32, ctypes.c_float, ctypes.c_float, vp, vp, i32, ctypes.c_float,
                              vp, u64, vp]
     lib.lrbi_lstm_step.argtypes = [pd, ctypes.c_int, vp, i64, vp, vp, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, u64, vp]
-    for name in ("lrbi_index_bits", "lrbi_index_bits_ranked", "lrbi_pack_factors_ranked", "lrbi_csr_bits",
+    lib.lrbi_quant_pack.argtypes = [pd, ctypes.c_int, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+    lib.lrbi_quant_unpack.argtypes = [ctypes.c_int, vp, i64, vp, i64, i64, i64, vp, i64, vp]
+    lib.lrbi_quant_matvec.argtypes = [ctypes.c_int, vp, i64, vp, i64, i64, i64, vp, i64, i64, vp, i64, vp]
+    lib.lrbi_checkpoint_pack.argtypes = [ctypes.c_int, vp, i64, i64, i64, vp, i64, vp, i64, vp]
+    lib.lrbi_checkpoint_unpack.argtypes = [ctypes.c_int, vp, i64, vp, i64, i64, i64, vp, i64, vp]
+    lib.lrbi_checkpoint_grad.argtypes = [pd, ctypes.c_int, vp, i64, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp]
+    lib.lrbi_token_logprobs_workspace_bytes.argtypes = [ctypes.c_int, i64, i64, i32, pu64]
+    lib.lrbi_token_logprobs.argtypes = [ctypes.c_int, vp, i64, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp, u64, vp]
+    lib.lrbi_token_logprobs_grad.argtypes = [ctypes.c_int, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    for name in ("lrbi_quant_pack", "lrbi_quant_unpack", "lrbi_quant_matvec", "lrbi_checkpoint_pack", "lrbi_checkpoint_unpack",
+                 "lrbi_checkpoint_grad", "lrbi_token_logprobs_workspace_bytes", "lrbi_token_logprobs", "lrbi_token_logprobs_grad",
+                 "lrbi_index_bits", "lrbi_index_bits_ranked", "lrbi_pack_factors_ranked", "lrbi_csr_bits",
                  "lrbi_pack_factors", "lrbi_unpack_mask", "lrbi_decode_mask",
                  "lrbi_masked_gemm_workspace_bytes", "lrbi_masked_gemm", "lrbi_masked_gemm_static", "lrbi_threshold_eval",
                  "lrbi_threshold_eval_workspace_bytes", "lrbi_search_thresholds", "lrbi_search_workspace_bytes",
@@ -546,3 +558,203 @@ def nmf(desc: Desc, W, Mp, Mz, iters: int, eps: float = 1e-9, method: int = 1, w
         _dev_ptr(Mp, "Mp"), _dev_ptr(Mz, "Mz"), int(iters), float(eps), _dev_ptr(workspace, "workspace"),
         workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "lrbi_nmf")
     return Mp, Mz
+
+
+def _store(out, rows, cols, block_bytes, device):
+    """Codes and scales of the block formats: the pair given, or new ones with the smallest pitches."""
+    blocks = -(-cols // 32)
+    if out is None:
+        import torch
+        return (torch.empty((rows, block_bytes * blocks), dtype=torch.uint8, device=device),
+                torch.empty((rows, -(-blocks // 4) * 4), dtype=torch.uint8, device=device))
+    codes, scales = out
+    if codes.shape[0] != rows or scales.shape[0] != rows:
+        raise ValueError("codes and scales must have a row for each row")
+    return codes, scales
+
+
+def _bytes(t, what):
+    """Address and row pitch of a matrix of bytes."""
+    if t.element_size() != 1 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a row-major matrix of bytes" % what)
+    # a tensor of one row may have any stride; its pitch is what it holds
+    return _dev_ptr(t, what), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _store_width(codes, scales, cols, block_bytes):
+    """Both hold what `cols` values of a row take."""
+    blocks = -(-cols // 32)
+    if codes.shape[1] < block_bytes * blocks or scales.shape[1] < blocks:
+        raise ValueError("codes or scales have too few columns")
+
+
+def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
+    """lrbi_quant_pack: W [m, n] with its pruned weights as zeros into 4-bit codes (uint8 [m, 16 per 32 columns]) and scale
+    bytes (uint8 [m, 1 per 32 columns, rows of 4-byte pieces]).  Without factors nothing is pruned.  `out` = (codes, scales)
+    reuses two tensors.  Returns (codes, scales)."""
+    if W.dim() != 2 or W.shape != (desc.m, desc.n) or (desc.n > 1 and W.stride(1) != 1):
+        raise ValueError("W must be a row-major [m, n] tensor")
+    codes, scales = _store(out, desc.m, desc.n, 16, W.device)
+    _store_width(codes, scales, desc.n, 16)
+    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    _check(load_library().lrbi_quant_pack(
+        ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), W.stride(0), None if dIp is None else _dev_ptr(dIp, "Ip"),
+        None if dIz is None else _dev_ptr(dIz, "Iz"), cp, ldc, sp, lds, _stream_ptr(stream)), "lrbi_quant_pack")
+    return codes, scales
+
+
+def _values_out(out, rows, cols, dtype, device):
+    if out is None:
+        import torch
+        return torch.empty((rows, cols), dtype=dtype, device=device)
+    if out.shape != (rows, cols) or out.dtype != dtype or (cols > 1 and out.stride(1) != 1):
+        raise ValueError("bad out tensor")
+    return out
+
+
+def quant_unpack(codes, scales, n: int, dtype, out=None, stream=None):
+    """lrbi_quant_unpack: the values [m, n] of 4-bit codes, as numbers of `dtype`."""
+    m = codes.shape[0]
+    out = _values_out(out, m, n, dtype, codes.device)
+    _store((codes, scales), m, n, 16, None)
+    _store_width(codes, scales, n, 16)
+    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _dev_ptr(out, "W"), out.stride(0),
+                                            _stream_ptr(stream)), "lrbi_quant_unpack")
+    return out
+
+
+def quant_matvec(codes, scales, X, out=None, stream=None):
+    """lrbi_quant_matvec: Y [m, N] = Wq X with the values Wq [m, n] of 4-bit codes and scales, X [n, N] (or [n])."""
+    squeeze = X.dim() == 1
+    if squeeze:
+        X = X.unsqueeze(1)
+    m, (n, N) = codes.shape[0], X.shape
+    ldx, x1 = X.stride()
+    if N > 1 and x1 != 1:
+        raise ValueError("X must be a row-major tensor")
+    if scales.shape[0] != m:
+        raise ValueError("codes and scales must have a row for each row")
+    _store_width(codes, scales, n, 16)
+    if squeeze and out is not None:
+        out = out.unsqueeze(1)
+    out, ldy = _row_major_out(out, m, N, X)
+    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    _check(load_library().lrbi_quant_matvec(_dtype_code(X), cp, ldc, sp, lds, m, n, _dev_ptr(X, "X"), ldx, N, _dev_ptr(out, "Y"), ldy,
+                                            _stream_ptr(stream)), "lrbi_quant_matvec")
+    return out[:, 0] if squeeze else out
+
+
+def checkpoint_pack(X, out=None, stream=None):
+    """lrbi_checkpoint_pack: a layer input X [n, N] into 8-bit codes (uint8 [n, N rounded up to 32]) and scale bytes (uint8
+    [n, 1 per 32 columns, rows of 4-byte pieces]).  `out` = (codes, scales) reuses two tensors.  Returns (codes, scales)."""
+    if X.dim() != 2 or (X.shape[1] > 1 and X.stride(1) != 1):
+        raise ValueError("X must be a row-major [n, N] tensor")
+    n, N = X.shape
+    codes, scales = _store(out, n, N, 32, X.device)
+    _store_width(codes, scales, N, 32)
+    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), _dev_ptr(X, "X"), X.stride(0), n, N, cp, ldc, sp, lds,
+                                               _stream_ptr(stream)), "lrbi_checkpoint_pack")
+    return codes, scales
+
+
+def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
+    """lrbi_checkpoint_unpack: the values [n, N] of a checkpoint, as numbers of `dtype`."""
+    n = codes.shape[0]
+    out = _values_out(out, n, N, dtype, codes.device)
+    _store((codes, scales), n, N, 32, None)
+    _store_width(codes, scales, N, 32)
+    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _dev_ptr(out, "X"), out.stride(0),
+                                                 _stream_ptr(stream)), "lrbi_checkpoint_unpack")
+    return out
+
+
+def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=None):
+    """lrbi_checkpoint_grad: masked_grad with X given as a checkpoint: dW = (dY Xq^T) o decode(Ip, Iz), dY [m, N]."""
+    m, n = desc.m, desc.n
+    if dY.dim() != 2 or dY.shape[0] != m or codes.shape[0] != n or scales.shape[0] != n:
+        raise ValueError("shape mismatch")
+    N = dY.shape[1]
+    if N > 1 and dY.stride(1) != 1:
+        raise ValueError("dY must be a row-major tensor")
+    _store_width(codes, scales, N, 32)
+    out, lddw = _row_major_out(out, m, n, dY)
+    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    _check(load_library().lrbi_checkpoint_grad(
+        ctypes.byref(desc), _dtype_code(dY), _dev_ptr(dY, "dY"), dY.stride(0), cp, ldc, sp, lds, N, _dev_ptr(dIp, "Ip"),
+        _dev_ptr(dIz, "Iz"), _dev_ptr(out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
+    return out
+
+
+MAX_TOP = 64
+
+# logp [N] (None without tokens), entropy [N], stats [2, N] float32; top_ids [top, N] int64, top_logp [top, N] float32 (None at top = 0)
+TokenLogprobs = namedtuple("TokenLogprobs", "logp entropy stats top_ids top_logp")
+
+
+def token_logprobs_workspace_bytes(dtype_code: int, V: int, N: int, top: int = 0) -> int:
+    out = ctypes.c_uint64()
+    _check(load_library().lrbi_token_logprobs_workspace_bytes(int(dtype_code), int(V), int(N), int(top), ctypes.byref(out)),
+           "lrbi_token_logprobs_workspace_bytes")
+    return out.value
+
+
+def _tokens_ptr(tokens, N):
+    import torch
+    if tokens.dtype != torch.int64 or tokens.shape != (N,) or not tokens.is_contiguous():
+        raise ValueError("tokens must be a contiguous int64 [N] tensor")
+    return _dev_ptr(tokens, "tokens")
+
+
+def _row_ptr(t, shape, what):
+    import torch
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous float32 tensor of shape %s" % (what, shape))
+    return _dev_ptr(t, what)
+
+
+def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, stream=None):
+    """lrbi_token_logprobs: logits [V, N] (row = word, column = token; what masked_gemm returns), tokens int64 [N] (negative:
+    padding).  Returns TokenLogprobs; `out` = an earlier call's result of the same shape, which is filled again.  `workspace`:
+    device scratch of at least token_logprobs_workspace_bytes bytes (allocated here when None)."""
+    import torch
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a row-major [V, N] tensor")
+    V, N = logits.shape
+    dev, code = logits.device, _dtype_code(logits)
+    if out is None:
+        new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)  # noqa: E731
+        out = TokenLogprobs(None if tokens is None else new(N), new(N), new(2, N),
+                            torch.empty((top, N), dtype=torch.int64, device=dev) if top > 0 else None, new(top, N) if top > 0 else None)
+    if (out.logp is None) != (tokens is None) or (out.top_ids is None) != (top <= 0):
+        raise ValueError("out is of a call with other results")
+    if workspace is None:
+        workspace = torch.empty(token_logprobs_workspace_bytes(code, V, N, top), dtype=torch.uint8, device=dev)
+    if top > 0 and (out.top_ids.shape != (top, N) or out.top_ids.dtype != torch.int64 or not out.top_ids.is_contiguous()):
+        raise ValueError("out.top_ids must be a contiguous int64 [top, N] tensor")
+    ws_ptr, ws_bytes = _scratch(workspace)
+    _check(load_library().lrbi_token_logprobs(
+        code, _dev_ptr(logits, "logits"), logits.stride(0), V, N, None if tokens is None else _tokens_ptr(tokens, N),
+        None if tokens is None else _row_ptr(out.logp, (N,), "out.logp"), _row_ptr(out.entropy, (N,), "out.entropy"),
+        _row_ptr(out.stats, (2, N), "out.stats"), top, _dev_ptr(out.top_ids, "out.top_ids") if top > 0 else None,
+        _row_ptr(out.top_logp, (top, N), "out.top_logp") if top > 0 else None, ws_ptr, ws_bytes, _stream_ptr(stream)),
+        "lrbi_token_logprobs")
+    return out
+
+
+def token_logprobs_grad(logits, tokens, result, g_logp=None, g_entropy=None, out=None, stream=None):
+    """lrbi_token_logprobs_grad: the gradient [V, N] of sum(g_logp * logp + g_entropy * entropy) with respect to the logits,
+    from the TokenLogprobs that token_logprobs gave for them.  g_logp, g_entropy: float32 [N], one of them may be None.
+    `out` may be `logits` itself."""
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a row-major [V, N] tensor")
+    V, N = logits.shape
+    out, lddl = _row_major_out(out, V, N, logits)
+    _check(load_library().lrbi_token_logprobs_grad(
+        _dtype_code(logits), _dev_ptr(logits, "logits"), logits.stride(0), V, N, None if tokens is None else _tokens_ptr(tokens, N),
+        _row_ptr(result.stats, (2, N), "stats"), _row_ptr(result.entropy, (N,), "entropy"),
+        None if g_logp is None else _row_ptr(g_logp, (N,), "g_logp"), None if g_entropy is None else _row_ptr(g_entropy, (N,), "g_entropy"),
+        _dev_ptr(out, "out"), lddl, _stream_ptr(stream)), "lrbi_token_logprobs_grad")
+    return out

@@ -631,7 +631,7 @@ extern "C" int lrbi_masked_grad(const lrbi_desc *desc, lrbi_dtype dtype, const v
     const Geom g = make_geom(desc);
     // matrix cores for every type at any batch (below 8 columns the slab is mostly zero fill); dW rows need not be 16-byte
     // aligned (the kernel then writes element by element)
-    return launch_grad(g, dtype, dDY, lddy, dX, ldx, N, (const uint32_t *)dIp_packed,
+    return launch_grad(g, dtype, dDY, lddy, dX, ldx, nullptr, 0, N, (const uint32_t *)dIp_packed,
                        (const uint32_t *)dIz_packed, dDW, lddw, (hipStream_t)stream);
 }
 
@@ -736,4 +736,148 @@ extern "C" int lrbi_nmf(const lrbi_desc *desc, lrbi_dtype dtype, const void *dW,
     if (iters == 0) return LRBI_OK;
     return launch_nmf(g, dtype, dW, ldw, method, w_threshold, amplify, dMp, dMz, iters, eps, dWorkspace,
                       (hipStream_t)stream);
+}
+
+static constexpr int64_t kMost = 0x7FFFFF00; // rows, columns
+
+// codes and scales of the block formats: whole blocks of `block_bytes` bytes, 16-byte aligned rows of codes, 4-byte aligned rows of scales
+static int check_store(const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t cols, int block_bytes)
+{
+    const int64_t blocks = (cols + 31) / 32;
+    if (ldc < blocks * block_bytes || ldc % 16 != 0 || lds < blocks || lds % 4 != 0) return LRBI_ERR_PITCH;
+    if (!aligned_to(dCodes, 16) || !aligned_to(dScales, 4)) return LRBI_ERR_ALIGN;
+    return LRBI_OK;
+}
+
+extern "C" int lrbi_quant_pack(const lrbi_desc *desc, lrbi_dtype dtype, const void *dW, int64_t ldw, const void *dIp_packed,
+                               const void *dIz_packed, void *dCodes, int64_t ldc, void *dScales, int64_t lds, void *stream)
+{
+    const int rc = validate_desc(desc);
+    if (rc != LRBI_OK) return rc;
+    if (!dW || !dCodes || !dScales || !dIp_packed != !dIz_packed) return LRBI_ERR_NULL;
+    const int es = elem_size(dtype);
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (ldw < desc->n) return LRBI_ERR_PITCH;
+    if (!aligned_to(dW, (uintptr_t)es) || !aligned_to(dIp_packed, 4) || !aligned_to(dIz_packed, 8)) return LRBI_ERR_ALIGN;
+    const int rs = check_store(dCodes, ldc, dScales, lds, desc->n, 16);
+    if (rs != LRBI_OK) return rs;
+    return launch_quant_pack(make_geom(desc), dtype, dW, ldw, (const uint32_t *)dIp_packed, (const uint32_t *)dIz_packed, dCodes, ldc,
+                             dScales, lds, (hipStream_t)stream);
+}
+
+extern "C" int lrbi_quant_unpack(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m, int64_t n,
+                                 void *dW, int64_t ldw, void *stream)
+{
+    if (!dW || !dCodes || !dScales) return LRBI_ERR_NULL;
+    const int es = elem_size(dtype);
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (m <= 0 || n <= 0 || m > kMost || n > kMost) return LRBI_ERR_SHAPE;
+    if (ldw < n) return LRBI_ERR_PITCH;
+    if (!aligned_to(dW, (uintptr_t)es)) return LRBI_ERR_ALIGN;
+    const int rs = check_store(dCodes, ldc, dScales, lds, n, 16);
+    if (rs != LRBI_OK) return rs;
+    return launch_quant_unpack(dtype, dCodes, ldc, dScales, lds, m, n, dW, ldw, (hipStream_t)stream);
+}
+
+extern "C" int lrbi_quant_matvec(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m, int64_t n,
+                                 const void *dX, int64_t ldx, int64_t N, void *dY, int64_t ldy, void *stream)
+{
+    if (!dX || !dY || !dCodes || !dScales) return LRBI_ERR_NULL;
+    const int es = elem_size(dtype);
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (m <= 0 || n <= 0 || N <= 0 || m > kMost || n > kMost || N > kMost) return LRBI_ERR_SHAPE;
+    if (ldx < N || ldy < N) return LRBI_ERR_PITCH;
+    if (!aligned_to(dX, (uintptr_t)es) || !aligned_to(dY, (uintptr_t)es)) return LRBI_ERR_ALIGN;
+    const int rs = check_store(dCodes, ldc, dScales, lds, n, 16);
+    if (rs != LRBI_OK) return rs;
+    return launch_quant_matvec(dtype, dCodes, ldc, dScales, lds, m, n, dX, ldx, N, dY, ldy, (hipStream_t)stream);
+}
+
+extern "C" int lrbi_checkpoint_pack(lrbi_dtype dtype, const void *dX, int64_t ldx, int64_t n, int64_t N, void *dCodes, int64_t ldc,
+                                    void *dScales, int64_t lds, void *stream)
+{
+    if (!dX || !dCodes || !dScales) return LRBI_ERR_NULL;
+    const int es = elem_size(dtype);
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (n <= 0 || N <= 0 || n > kMost || N > kMost) return LRBI_ERR_SHAPE;
+    if (ldx < N) return LRBI_ERR_PITCH;
+    if (!aligned_to(dX, (uintptr_t)es)) return LRBI_ERR_ALIGN;
+    const int rs = check_store(dCodes, ldc, dScales, lds, N, 32);
+    if (rs != LRBI_OK) return rs;
+    return launch_checkpoint_pack(dtype, dX, ldx, n, N, dCodes, ldc, dScales, lds, (hipStream_t)stream);
+}
+
+extern "C" int lrbi_checkpoint_unpack(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t n,
+                                      int64_t N, void *dX, int64_t ldx, void *stream)
+{
+    if (!dX || !dCodes || !dScales) return LRBI_ERR_NULL;
+    const int es = elem_size(dtype);
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (n <= 0 || N <= 0 || n > kMost || N > kMost) return LRBI_ERR_SHAPE;
+    if (ldx < N) return LRBI_ERR_PITCH;
+    if (!aligned_to(dX, (uintptr_t)es)) return LRBI_ERR_ALIGN;
+    const int rs = check_store(dCodes, ldc, dScales, lds, N, 32);
+    if (rs != LRBI_OK) return rs;
+    return launch_checkpoint_unpack(dtype, dCodes, ldc, dScales, lds, n, N, dX, ldx, (hipStream_t)stream);
+}
+
+extern "C" int lrbi_checkpoint_grad(const lrbi_desc *desc, lrbi_dtype dtype, const void *dDY, int64_t lddy, const void *dCodes, int64_t ldc,
+                                    const void *dScales, int64_t lds, int64_t N, const void *dIp_packed, const void *dIz_packed, void *dDW,
+                                    int64_t lddw, void *stream)
+{
+    const int rc = validate_desc(desc);
+    if (rc != LRBI_OK) return rc;
+    if (!dDY || !dCodes || !dScales || !dIp_packed || !dIz_packed || !dDW) return LRBI_ERR_NULL;
+    const int es = elem_size(dtype);
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (N <= 0 || N > kMost) return LRBI_ERR_SHAPE;
+    if (lddw < desc->n || lddy < N) return LRBI_ERR_PITCH;
+    if (!aligned_to(dIp_packed, 4) || !aligned_to(dIz_packed, 8)) return LRBI_ERR_ALIGN;
+    if (!aligned_to(dDW, (uintptr_t)es) || !aligned_to(dDY, (uintptr_t)es)) return LRBI_ERR_ALIGN;
+    const int rs = check_store(dCodes, ldc, dScales, lds, N, 32);
+    if (rs != LRBI_OK) return rs;
+    return launch_grad(make_geom(desc), dtype, dDY, lddy, dCodes, ldc, dScales, lds, N, (const uint32_t *)dIp_packed,
+                       (const uint32_t *)dIz_packed, dDW, lddw, (hipStream_t)stream);
+}
+
+extern "C" int lrbi_token_logprobs_workspace_bytes(lrbi_dtype dtype, int64_t V, int64_t N, int32_t top, uint64_t *bytes)
+{
+    if (!bytes) return LRBI_ERR_NULL;
+    const int es = elem_size(dtype);
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (V <= 0 || N <= 0 || V > kMost || N > kMost || top < 0 || top > LRBI_MAX_TOP) return LRBI_ERR_SHAPE;
+    *bytes = logprobs_workspace_bytes(es, V, N, top);
+    return LRBI_OK;
+}
+
+extern "C" int lrbi_token_logprobs(lrbi_dtype dtype, const void *dL, int64_t ldl, int64_t V, int64_t N, const int64_t *dTok, float *dLogp,
+                                   float *dEntropy, float *dStats, int32_t top, int64_t *dTopIds, float *dTopLogp, void *dWorkspace,
+                                   uint64_t workspace_bytes, void *stream)
+{
+    const int es = elem_size(dtype);
+    if (!dL || !dStats || !dWorkspace || !dTok != !dLogp) return LRBI_ERR_NULL;
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (V <= 0 || N <= 0 || V > kMost || N > kMost || top < 0 || top > LRBI_MAX_TOP) return LRBI_ERR_SHAPE;
+    if (top > 0 && (!dTopIds || !dTopLogp)) return LRBI_ERR_NULL;
+    if (ldl < N) return LRBI_ERR_PITCH;
+    if (!aligned_to(dL, (uintptr_t)es) || !aligned_to(dTok, 8) || !aligned_to(dLogp, 4) || !aligned_to(dEntropy, 4) ||
+        !aligned_to(dStats, 4) || !aligned_to(dTopIds, 8) || !aligned_to(dTopLogp, 4) || !aligned_to(dWorkspace, 16))
+        return LRBI_ERR_ALIGN;
+    if (workspace_bytes < logprobs_workspace_bytes(es, V, N, top)) return LRBI_ERR_WORKSPACE;
+    return launch_logprobs(dtype, dL, ldl, V, N, dTok, dLogp, dEntropy, dStats, top, dTopIds, dTopLogp, dWorkspace, (hipStream_t)stream);
+}
+
+extern "C" int lrbi_token_logprobs_grad(lrbi_dtype dtype, const void *dL, int64_t ldl, int64_t V, int64_t N, const int64_t *dTok,
+                                        const float *dStats, const float *dEntropy, const float *dGLogp, const float *dGEntropy, void *dDL,
+                                        int64_t lddl, void *stream)
+{
+    const int es = elem_size(dtype);
+    if (!dL || !dStats || !dDL || (!dGLogp && !dGEntropy) || (dGLogp && !dTok) || (dGEntropy && !dEntropy)) return LRBI_ERR_NULL;
+    if (es == 0) return LRBI_ERR_DTYPE;
+    if (V <= 0 || N <= 0 || V > kMost || N > kMost) return LRBI_ERR_SHAPE;
+    if (ldl < N || lddl < N) return LRBI_ERR_PITCH;
+    if (!aligned_to(dL, (uintptr_t)es) || !aligned_to(dDL, (uintptr_t)es) || !aligned_to(dTok, 8) || !aligned_to(dStats, 4) ||
+        !aligned_to(dEntropy, 4) || !aligned_to(dGLogp, 4) || !aligned_to(dGEntropy, 4))
+        return LRBI_ERR_ALIGN;
+    return launch_logprobs_grad(dtype, dL, ldl, V, N, dTok, dStats, dEntropy, dGLogp, dGEntropy, dDL, lddl, (hipStream_t)stream);
 }

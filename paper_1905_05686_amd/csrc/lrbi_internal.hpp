@@ -57,8 +57,9 @@ int launch_f32_gemm(const Geom &g, const float *dW, int64_t ldw, const uint32_t 
                     int64_t ldx, int64_t N, float *dY, int64_t ldy, hipStream_t stream);
 int launch_f32_gemm_t(const Geom &g, lrbi_dtype dt, const void *dW, int64_t ldw, const uint32_t *dIp, const uint32_t *dIz,
                       const void *dDY, int64_t lddy, int64_t N, void *dDX, int64_t lddx, hipStream_t stream);
-int launch_f32_grad(const Geom &g, const float *dDY, int64_t lddy, const float *dX, int64_t ldx, int64_t N,
-                    const uint32_t *dIp, const uint32_t *dIz, float *dDW, int64_t lddw, hipStream_t stream);
+// (dXScales: NULL, or the scale bytes of an activation checkpoint whose codes dX are, here and in launch_grad)
+int launch_f32_grad(const Geom &g, const float *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales, int64_t ldxs,
+                    int64_t N, const uint32_t *dIp, const uint32_t *dIz, float *dDW, int64_t lddw, hipStream_t stream);
 
 // threshold search of Algorithm 1 (lrbi_alg1.hip): workspace layout (byte offsets) and sizes
 struct SearchPlan {
@@ -91,8 +92,8 @@ int pipe_t_slices(const Geom &g, int64_t N, int max_slices, int64_t *iper);
 int launch_pipe_t_gemm(const Geom &g, int slices, int64_t iper, lrbi_dtype dt, const void *dW, int64_t ldw,
                        const uint32_t *dIp, const uint32_t *dIz, const void *dDY, int64_t lddy, int64_t N, void *dDX,
                        int64_t lddx, void *dWorkspace, hipStream_t stream);
-int launch_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx,
-                int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream);
+int launch_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales,
+                int64_t ldxs, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream);
 
 // the weight gradient in 256 x 256 tiles (lrbi_grad256.hip): what it takes, and where it is the better choice
 bool grad256_ok(const Geom &g, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, int64_t N);
@@ -171,6 +172,28 @@ int launch_pipe256_gemm(const Geom &g, lrbi_dtype dt, const void *dW, int64_t ld
 uint64_t nmf_workspace_bytes(const Geom &g);
 int launch_nmf(const Geom &g, lrbi_dtype dt, const void *dW, int64_t ldw, int method, float w_threshold, float amplify,
                float *dMp, float *dMz, int iters, float eps, void *dWorkspace, hipStream_t stream);
+
+// weights in 4 bits (lrbi_quant.hip); dIp, dIz both NULL: nothing is pruned
+int launch_quant_pack(const Geom &g, lrbi_dtype dt, const void *dW, int64_t ldw, const uint32_t *dIp, const uint32_t *dIz, void *dCodes,
+                      int64_t ldc, void *dScales, int64_t lds, hipStream_t stream);
+int launch_quant_unpack(lrbi_dtype dt, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m, int64_t n, void *dW,
+                        int64_t ldw, hipStream_t stream);
+int launch_quant_matvec(lrbi_dtype dt, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m, int64_t n,
+                        const void *dX, int64_t ldx, int64_t N, void *dY, int64_t ldy, hipStream_t stream);
+
+// activation checkpoints in 8 bits (lrbi_checkpoint.hip)
+int launch_checkpoint_pack(lrbi_dtype dt, const void *dX, int64_t ldx, int64_t n, int64_t N, void *dCodes, int64_t ldc, void *dScales,
+                           int64_t lds, hipStream_t stream);
+int launch_checkpoint_unpack(lrbi_dtype dt, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t n, int64_t N,
+                             void *dX, int64_t ldx, hipStream_t stream);
+
+// token log probabilities and their gradient (lrbi_logprobs.hip)
+uint64_t logprobs_workspace_bytes(int elem_size, int64_t V, int64_t N, int32_t top);
+int launch_logprobs(lrbi_dtype dt, const void *dL, int64_t ldl, int64_t V, int64_t N, const int64_t *dTok, float *dLogp, float *dEntropy,
+                    float *dStats, int32_t top, int64_t *dTopIds, float *dTopLogp, void *ws, hipStream_t stream);
+int launch_logprobs_grad(lrbi_dtype dt, const void *dL, int64_t ldl, int64_t V, int64_t N, const int64_t *dTok, const float *dStats,
+                         const float *dEntropy, const float *dGLogp, const float *dGEntropy, void *dDL, int64_t lddl,
+                         hipStream_t stream);
 
 // LSTM cell on the fp32 planes of a gate product (lrbi_lstm.hip)
 int launch_lstm_cell(lrbi_dtype dt, const float *dPlanes, int slices, int64_t m, int64_t ldp, int64_t B, float *dC,
