@@ -12,12 +12,16 @@
 // type's lowest value and nothing else): there c = 1.  Neighbouring numbers are at least 64 apart, so that e^d and 2^d are both
 // 1 at the maximum and nothing elsewhere.
 //
-// Top words.  The rows are cut into runs of 32; the first kernel leaves the maximum of every run and column.  A word that
-// belongs to the top K lies in a run whose maximum is not below the K-th largest of any K or more such maxima: the
-// finishing wavefront takes the 64 maxima of its lanes' runs, their K-th largest as a bound, reads the few runs that reach it
-// and ranks the words that reach it by counting.
+// Top words.  The rows are cut into runs of 32; the first kernel leaves the largest logit of every run and column, its row, and
+// the second largest.  A word that belongs to the top K lies in a run whose maximum is not below the K-th largest of any K or
+// more such maxima: the finishing wavefront takes the maxima of its 64 lanes' runs and their K-th largest as a bound.  The few
+// runs that reach it give their largest word; only those whose second largest reaches it too are read again.  The words
+// found are ranked by counting.  (Reading every run that reaches the bound: 65536 words, 256 tokens, 20 top words 32 us
+// against 22.)
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
+
+#include <type_traits>
 
 #include "lrbi_internal.hpp"
 
@@ -26,6 +30,7 @@ namespace lrbi {
 static constexpr int LP_THREADS = 256;
 static constexpr int LP_BATCH = 16; // rows whose maximum is taken before their exponentials
 static constexpr int LP_RUN = 32;   // rows per run of the top words
+static constexpr int LP_GRAD = 8;   // rows of a batch of the gradient
 static constexpr float LP_LOG2E = 1.44269504088896f, LP_LN2 = 0.693147180559945f;
 static constexpr float LP_HUGE = 0x1p30f;
 
@@ -46,7 +51,7 @@ template <> struct Logit<__hip_bfloat16> {
     static constexpr bool can_be_huge = true;
     static constexpr float lowest = -0x1.fffffep127f; // every finite number of the type is at least this
     __device__ static float widen(__hip_bfloat16 v) { return __bfloat162float(v); }
-    __device__ static __hip_bfloat16 narrow(float v) { return __float2bfloat16(v); }
+    __device__ static __hip_bfloat16 narrow(float v) { return __builtin_bit_cast(__hip_bfloat16, (__bf16)v); } // nearest-even
 };
 
 // P values of a row as one load or store
@@ -91,67 +96,140 @@ template <typename T> __device__ __forceinline__ LpSums lp_join(LpSums a, LpSums
     return a;
 }
 
+// Rows of P columns from `src` on, rows ldl apart; COLUMN: the logits are one column without gaps (P = 1), read as
+// 16-byte pieces.
+template <typename T, int P, bool COLUMN, int ROWS>
+__device__ __forceinline__ void lp_load(Piece<T, P> (&x)[ROWS], const T *src, int64_t ldl, int left)
+{
+    if (left < ROWS) { // past the last row: words of probability 0
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            if (i < left) {
+                x[i] = *reinterpret_cast<const Piece<T, P> *>(src + i * ldl);
+            } else {
+#pragma unroll
+                for (int p = 0; p < P; ++p) x[i].v[p] = Logit<T>::narrow(-__builtin_inff());
+            }
+        }
+    } else if constexpr (COLUMN) {
+        constexpr int N16 = ROWS * sizeof(T) / 16;
+        uint4 v[N16];
+#pragma unroll
+        for (int i = 0; i < N16; ++i) v[i] = reinterpret_cast<const uint4 *>(src)[i];
+        __builtin_memcpy(x, v, sizeof(x));
+    } else {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) x[i] = *reinterpret_cast<const Piece<T, P> *>(src + i * ldl);
+    }
+}
+
+// The second largest logit of a run, rounded up to 27 bits, and the row of the largest in the other five.
+__device__ __forceinline__ uint32_t lp_more(float second, int row)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, second);
+    // a positive number with its last five bits set is not smaller, a negative one with them cleared not larger
+    return (((u >> 31) ? u : u + 31u) & ~31u) | (uint32_t)row;
+}
+// (a second largest that is +infinity stays one; what is rounded up past the largest number is read again for nothing)
+__device__ __forceinline__ float lp_second(uint32_t more) { return __builtin_bit_cast(float, more & ~31u); }
+
 // One pass: lane (tx, ty) of a workgroup takes columns (block * tx_count + tx) P .. + P - 1 and the `runs` runs of 32 rows
-// from ((slice * ty_count) + ty) * runs on.  part: [slice][3][N].  run_max: [run][N], or NULL.
-template <typename T, int P>
+// from ((slice * ty_count) + ty) * runs on.  part: [column][slice]; TOP: run_max, run_more: [column][run_pitch].
+template <typename T, int P, bool COLUMN, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N,
-                                                                   int tx_count, int ty_count, int64_t runs, int64_t slices,
-                                                                   float *__restrict__ part, float *__restrict__ run_max)
+                                                                   int tx_count, int ty_count, int64_t col_blocks, int64_t runs, int64_t slices,
+                                                                   float4 *__restrict__ part, float *__restrict__ run_max,
+                                                                   uint32_t *__restrict__ run_more, int64_t run_pitch)
 {
     __shared__ float join[3 * P][LP_THREADS];
     const int tid = threadIdx.x;
     const int ty = tid / tx_count, tx = tid - ty * tx_count;
     const int64_t blk = wide_block();
-    const int64_t cb = blk / slices, slice = blk - cb * slices;
+    const int64_t slice = blk / col_blocks, cb = blk - slice * col_blocks; // neighbours read the same rows
     const int64_t q0 = (cb * tx_count + tx) * P;
-    if (cb * tx_count * P >= N) return; // a workgroup past the last one
+    if (slice >= slices) return; // a workgroup past the last one
     LpSums a[P];
+    float top[P]; // of the current run, and more of it
+    uint32_t more[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) a[p] = lp_empty<T>();
     if (ty < ty_count && q0 < N) {
         const int64_t run0 = (slice * ty_count + ty) * runs;
         for (int64_t run = run0; run < run0 + runs && run * LP_RUN < V; ++run) {
-            float top[P];
+            float second[P];
+            int at[P];
+            if constexpr (TOP)
 #pragma unroll
-            for (int p = 0; p < P; ++p) top[p] = -__builtin_inff();
+                for (int p = 0; p < P; ++p) {
+                    top[p] = second[p] = -__builtin_inff();
+                    at[p] = 0;
+                }
 #pragma unroll 1
             for (int h = 0; h < LP_RUN; h += LP_BATCH) {
                 const int64_t v0 = run * LP_RUN + h;
                 if (v0 >= V) break;
-                const T *src = L + v0 * ldl + q0;
-                Piece<T, P> x[LP_BATCH];
                 const int left = V - v0 < LP_BATCH ? (int)(V - v0) : LP_BATCH;
-                if (left == LP_BATCH) {
-#pragma unroll
-                    for (int i = 0; i < LP_BATCH; ++i) x[i] = *reinterpret_cast<const Piece<T, P> *>(src + i * ldl);
-                } else { // past the last row: the last one again, and not counted
-#pragma unroll
-                    for (int i = 0; i < LP_BATCH; ++i)
-                        x[i] = *reinterpret_cast<const Piece<T, P> *>(src + (i < left ? i : left - 1) * ldl);
-                }
+                Piece<T, P> x[LP_BATCH];
+                lp_load<T, P, COLUMN, LP_BATCH>(x, L + v0 * ldl + q0, ldl, left);
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     float b = Logit<T>::widen(x[0].v[p]);
+                    if constexpr (TOP) {
+                        float b2 = -__builtin_inff(); // the middle one of (x, largest, second) is the new second
 #pragma unroll
-                    for (int i = 1; i < LP_BATCH; ++i) b = fmaxf(b, Logit<T>::widen(x[i].v[p]));
-                    top[p] = fmaxf(top[p], b);
+                        for (int i = 1; i < LP_BATCH; ++i) {
+                            const float v = Logit<T>::widen(x[i].v[p]);
+                            b2 = __builtin_amdgcn_fmed3f(v, b, b2);
+                            b = fmaxf(b, v);
+                        }
+                        int row = 0;
+#pragma unroll
+                        for (int i = LP_BATCH - 1; i >= 0; --i) row = Logit<T>::widen(x[i].v[p]) == b ? i : row;
+                        second[p] = fmaxf(fmaxf(second[p], b2), fminf(top[p], b));
+                        at[p] = b > top[p] ? h + row : at[p];
+                        top[p] = fmaxf(top[p], b);
+                    } else {
+#pragma unroll
+                        for (int i = 1; i < LP_BATCH; ++i) b = fmaxf(b, Logit<T>::widen(x[i].v[p]));
+                    }
                     const float m = fmaxf(a[p].m, b), c = lp_factor<T>(m), r = m * c;
                     lp_raise(a[p], m, c, r);
 #pragma unroll
                     for (int i = 0; i < LP_BATCH; ++i) {
                         const float d = __builtin_fmaf(Logit<T>::widen(x[i].v[p]), c, -r);
-                        float e = lp_exp2(d);
-                        if (left != LP_BATCH && i >= left) e = 0.f;
+                        const float e = lp_exp2(d);
                         a[p].s += e;
                         a[p].t = __builtin_fmaf(lp_finite(d), e, a[p].t);
                     }
                 }
             }
-            if (run_max)
+            if constexpr (TOP)
 #pragma unroll
-                for (int p = 0; p < P; ++p)
-                    if (q0 + p < N) run_max[run * N + q0 + p] = top[p];
+                for (int p = 0; p < P; ++p) {
+                    more[p] = lp_more(second[p], at[p]);
+                    if (runs > 1) { // a lane's own runs lie side by side
+                        run_max[(q0 + p) * run_pitch + run] = top[p];
+                        run_more[(q0 + p) * run_pitch + run] = more[p];
+                    }
+                }
         }
+    }
+    if (TOP && runs == 1) { // one run a lane: those of a column together, so that its neighbours share a store
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            join[p][tid] = top[p];
+            join[P + p][tid] = __builtin_bit_cast(float, more[p]);
+        }
+        __syncthreads();
+        for (int e = tid; e < tx_count * P * ty_count; e += blockDim.x) {
+            const int col = e / ty_count, y = e - col * ty_count, from = y * tx_count + col / P;
+            const int64_t q = cb * tx_count * P + col, run = slice * ty_count + y;
+            if (q < N && run * LP_RUN < V) {
+                run_max[q * run_pitch + run] = join[col % P][from];
+                run_more[q * run_pitch + run] = __builtin_bit_cast(uint32_t, join[P + col % P][from]);
+            }
+        }
+        __syncthreads();
     }
     // the lanes that share a column: pairs ever closer together
 #pragma unroll
@@ -175,15 +253,9 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__re
             }
         }
     }
-    if (ty == 0)
+    if (ty == 0 && q0 < N)
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (q0 + p < N) {
-                float *o = part + slice * 3 * N + q0 + p;
-                o[0] = a[p].m;
-                o[N] = a[p].s;
-                o[2 * N] = a[p].t;
-            }
+        for (int p = 0; p < P; ++p) part[(q0 + p) * slices + slice] = make_float4(a[p].m, a[p].s, a[p].t, 0.f);
 }
 
 __device__ __forceinline__ void wave_sync()
@@ -192,262 +264,352 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-static constexpr int LP_LIST = 256; // words a wavefront holds at a time
-struct LpList {
-    float value[LP_LIST];
-    int64_t word[LP_LIST];
-    int64_t run[LP_THREADS]; // runs to read
+static constexpr int LP_LIST = 256;  // words a wavefront holds at a time
+static constexpr int LP_ROUND = 2048; // runs it looks at in a round: eight loads of four a lane, in flight together
+static constexpr int LP_AHEAD = LP_ROUND / 256;
+struct alignas(16) LpList {
+    uint64_t key[LP_LIST + 8]; // larger: the likelier word; all different
+    int run[LP_ROUND], again[64];
 };
-
-// The K best words of the list, sorted, at its start; the rest is dropped.  Returns how many there are.
-__device__ __forceinline__ int lp_rank(LpList &l, int count, int K, int lane)
+// a logit's place among the numbers (both zeros the same), then the lower word first
+__device__ __forceinline__ uint64_t lp_key(float x, int word)
 {
-    float v[LP_LIST / 64];
-    int64_t w[LP_LIST / 64];
-    int rank[LP_LIST / 64];
+    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);
+    return ((uint64_t)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32) | (uint32_t)~word;
+}
+__device__ __forceinline__ float lp_key_logit(uint64_t key)
+{
+    const uint32_t o = (uint32_t)(key >> 32);
+    return __builtin_bit_cast(float, o ^ ((o >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ int lp_key_word(uint64_t key) { return (int)~(uint32_t)key; }
+
+// The K largest keys of the list, sorted, at its start; the rest is dropped.  Returns how many there are.  A key's place is the
+// number of keys above it; PER keys a lane.
+template <int PER> __device__ __forceinline__ int lp_rank_of(LpList &l, int count, int K, int lane)
+{
+    wave_sync();
+    if (lane < 8) l.key[count + lane] = 0; // below every key
+    wave_sync();
+    uint64_t k[PER];
+    int rank[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        k[i] = lane + 64 * i < count ? l.key[lane + 64 * i] : 0;
+        rank[i] = 0;
+    }
+    for (int j = 0; j < count; j += 8) {
+        ulonglong2 o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = *reinterpret_cast<const ulonglong2 *>(&l.key[j + 2 * e]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) rank[i] += (o[e].x > k[i] ? 1 : 0) + (o[e].y > k[i] ? 1 : 0);
+    }
     wave_sync();
 #pragma unroll
-    for (int i = 0; i < LP_LIST / 64; ++i) {
-        const int at = lane + 64 * i;
-        v[i] = at < count ? l.value[at] : 0.f;
-        w[i] = at < count ? l.word[at] : 0;
-        rank[i] = at < count ? 0 : LP_LIST;
-    }
-    for (int j = 0; j < count; ++j) {
-        const float vj = l.value[j];
-        const int64_t wj = l.word[j];
-#pragma unroll
-        for (int i = 0; i < LP_LIST / 64; ++i) rank[i] += (vj > v[i] || (vj == v[i] && wj < w[i])) ? 1 : 0;
-    }
-    wave_sync();
-#pragma unroll
-    for (int i = 0; i < LP_LIST / 64; ++i)
-        if (rank[i] < K) {
-            l.value[rank[i]] = v[i];
-            l.word[rank[i]] = w[i];
-        }
+    for (int i = 0; i < PER; ++i)
+        if (k[i] && rank[i] < K) l.key[rank[i]] = k[i];
     wave_sync();
     return count < K ? count : K;
 }
+__device__ __forceinline__ int lp_rank(LpList &l, int count, int K, int lane)
+{
+    return count <= 64 ? lp_rank_of<1>(l, count, K, lane) : lp_rank_of<LP_LIST / 64>(l, count, K, lane);
+}
+
+// Four runs' maxima: -infinity past the last run
+__device__ __forceinline__ void lp_runs(float (&p)[4], const float *run_max, int i, int runs)
+{
+    const float none = -__builtin_inff();
+    const float4 v = i < runs ? *reinterpret_cast<const float4 *>(run_max + i) : make_float4(none, none, none, none);
+    p[0] = v.x;
+    p[1] = i + 1 < runs ? v.y : none;
+    p[2] = i + 2 < runs ? v.z : none;
+    p[3] = i + 3 < runs ? v.w : none;
+}
 
 // The K most likely words of column q, by one wavefront: sorted in `l`; returns how many there are (words at -infinity are
-// none, nor are NaN).
+// none, nor are NaN).  run_max: the column's runs, 16-byte aligned, room for a multiple of 4; piece: the first round of them,
+// run 256 k + 4 lane + e as piece[k][e].
 template <typename T>
-__device__ int lp_top(LpList &l, const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N, int64_t q, const float *__restrict__ run_max,
-                      int K, int lane)
+__device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_t ldl, int V, int64_t q, const float *__restrict__ run_max,
+                                      const uint32_t *__restrict__ run_more, int runs, float (&piece)[LP_AHEAD][4], int K, int lane)
 {
-    const int64_t runs = (V + LP_RUN - 1) / LP_RUN;
     const float none = -__builtin_inff();
     float mine = none;
-    for (int64_t i = lane; i < runs; i += 64) mine = fmaxf(mine, run_max[i * N + q]);
-    int rank = 0;
+    for (int i0 = 0;;) {
+#pragma unroll
+        for (int k = 0; k < LP_AHEAD; ++k) mine = fmaxf(mine, fmaxf(fmaxf(piece[k][0], piece[k][1]), fmaxf(piece[k][2], piece[k][3])));
+        i0 += LP_ROUND;
+        if (i0 >= runs) break;
+#pragma unroll
+        for (int k = 0; k < LP_AHEAD; ++k) lp_runs(piece[k], run_max, i0 + 256 * k + 4 * lane, runs);
+    }
+    // the K-th largest of the lanes' maxima: fewer than K are above it, K or more are not below it
+    int above = 0, not_below = 0;
+#pragma unroll
     for (int j = 0; j < 64; ++j) {
         const float v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), j));
-        rank += (v > mine || (v == mine && j < lane)) ? 1 : 0;
+        above += v > mine ? 1 : 0;
+        not_below += v >= mine ? 1 : 0;
     }
-    // a word below `bound` is behind K others; once K words are held, so is an equal one that comes later
-    float bound = __shfl(mine, __builtin_ctzll(__ballot(rank == K - 1)), 64);
-    bool full = false;
-    int count = 0, waiting = 0;
-    constexpr int LOADS = 8; // of two runs each, in flight together
-    auto read = [&]() {
-        wave_sync();
-        float v[LOADS];
-        int64_t w[LOADS];
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int at = 2 * u + (lane >> 5);
-            w[u] = at < waiting ? l.run[at] * LP_RUN + (lane & 31) : V;
-            v[u] = w[u] < V ? Logit<T>::widen(L[w[u] * ldl + q]) : none;
+    const float least = __shfl(mine, __builtin_ctzll(__ballot(above < K && not_below >= K)), 64);
+    // keys that are not above `bound` are behind K others, or of no word
+    const uint64_t lowest = lp_key(none, -1) | 0xFFFFFFFFu, at_least = lp_key(least, -1);
+    uint64_t bound = at_least > lowest ? at_least : lowest;
+    int count = 0;
+    const uint64_t below = (1ull << lane) - 1;
+    auto push = [&](uint64_t key, bool in) __attribute__((always_inline)) {
+        const uint64_t all = __ballot(in && key > bound);
+        if (!all) return;
+        if ((all >> lane) & 1) l.key[count + __builtin_popcountll(all & below)] = key;
+        count += __builtin_popcountll(all);
+        if (count > LP_LIST - 64) {
+            count = lp_rank_of<LP_LIST / 64>(l, count, K, lane);
+            if (count == K) bound = l.key[K - 1];
         }
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const uint64_t in = __ballot(v[u] > none && (full ? v[u] > bound : v[u] >= bound));
-            if (!in) continue;
-            if (count > LP_LIST - 64) {
-                count = lp_rank(l, count, K, lane);
-                if (count == K) {
-                    bound = l.value[K - 1];
-                    full = true;
-                }
-            }
-            if ((in >> lane) & 1) {
-                const int at = count + __builtin_popcountll(in & ((1ull << lane) - 1));
-                l.value[at] = v[u];
-                l.word[at] = w[u];
-            }
-            count += __builtin_popcountll(in);
-        }
-        // the runs that were not read move to the front
-        wave_sync();
-        const int64_t next = lane + 2 * LOADS < waiting ? l.run[lane + 2 * LOADS] : 0;
-        wave_sync();
-        l.run[lane] = next;
-        waiting = waiting > 2 * LOADS ? waiting - 2 * LOADS : 0;
     };
-    for (int64_t i0 = 0; i0 < runs; i0 += 64) {
-        const float v = i0 + lane < runs ? run_max[(i0 + lane) * N + q] : none;
-        const bool in = v > none && (full ? v > bound : v >= bound);
-        const uint64_t all = __ballot(in);
-        if (in) l.run[waiting + __builtin_popcountll(all & ((1ull << lane) - 1))] = i0 + lane;
-        waiting += __builtin_popcountll(all);
-        while (waiting >= 2 * LOADS) read();
+    for (int i0 = 0; i0 < runs; i0 += LP_ROUND) {
+        // the runs that reach the bound: each lane's behind those of the lanes before it
+        uint32_t hit = 0;
+#pragma unroll
+        for (int k = 0; k < LP_AHEAD; ++k) {
+            if (runs > LP_ROUND) lp_runs(piece[k], run_max, i0 + 256 * k + 4 * lane, runs); // otherwise they are there
+#pragma unroll
+            for (int e = 0; e < 4; ++e) hit |= piece[k][e] >= least && piece[k][e] > none ? 1u << (4 * k + e) : 0u;
+        }
+        int end = __builtin_popcount(hit);
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) {
+            const int before = __shfl_up(end, step, 64);
+            end += lane >= step ? before : 0;
+        }
+        const int found = __builtin_amdgcn_readlane(end, 63);
+        wave_sync();
+        for (int at = end - __builtin_popcount(hit); hit; hit &= hit - 1) {
+            const int bit = __builtin_ctz(hit);
+            l.run[at++] = i0 + 256 * (bit >> 2) + 4 * lane + (bit & 3);
+        }
+        wave_sync();
+        for (int from = 0; from < found; from += 64) {
+            const bool in = from + lane < found;
+            const int run = l.run[in ? from + lane : from];
+            const uint32_t more = run_more[run];
+            const int word = run * LP_RUN + (int)(more & 31u);
+            push(lp_key(run_max[run], word), in);
+            // second largest: at best the run's first word
+            const bool again = in && lp_second(more) > none && lp_key(lp_second(more), run * LP_RUN) > bound;
+            const uint64_t all = __ballot(again);
+            const int left = __builtin_popcountll(all);
+            if (!left) continue;
+            wave_sync();
+            if (again) l.again[__builtin_popcountll(all & below)] = word;
+            wave_sync();
+            constexpr int LOADS = 8; // of two runs each, in flight together
+            for (int a0 = 0; a0 < left; a0 += 2 * LOADS) {
+                float v[LOADS];
+                int w[LOADS];
+                bool is[LOADS];
+#pragma unroll
+                for (int u = 0; u < LOADS; ++u) {
+                    const int at = a0 + 2 * u + (lane >> 5), best = l.again[at < left ? at : 0];
+                    w[u] = best / LP_RUN * LP_RUN + (lane & 31);
+                    is[u] = at < left && w[u] < V && w[u] != best;
+                    v[u] = is[u] ? Logit<T>::widen(L[w[u] * ldl + q]) : none;
+                }
+#pragma unroll
+                for (int u = 0; u < LOADS; ++u) push(lp_key(v[u], w[u]), is[u] && v[u] > none);
+            }
+        }
     }
-    if (waiting) read();
     return lp_rank(l, count, K, lane);
 }
 
-// Joins the slices of 16 columns and writes their results; with TOP, wavefront w finds the top words of column w.
+// Joins a column's slices and writes its results, one wavefront a column.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(TOP ? 1024 : 256) void logprobs_finish_kernel(
-    const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N, const int64_t *__restrict__ tok, const float *__restrict__ part,
-    int64_t slices, const float *__restrict__ run_max, float *__restrict__ logp, float *__restrict__ entropy,
+__global__ __launch_bounds__(LP_THREADS) void logprobs_finish_kernel(
+    const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N, const int64_t *__restrict__ tok, const float4 *__restrict__ part,
+    int64_t slices, const float *__restrict__ run_max, const uint32_t *__restrict__ run_more, int64_t run_pitch, float *__restrict__ logp, float *__restrict__ entropy,
     float *__restrict__ stats, int K, int64_t *__restrict__ top_ids, float *__restrict__ top_logp)
 {
-    constexpr int THREADS = TOP ? 1024 : 256, WAVES = THREADS / 64;
-    __shared__ LpSums join[WAVES][16];
-    __shared__ float column[2][16]; // largest logit, ln of the sum
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t q0 = (int64_t)blockIdx.x * 16, q = q0 + (tid & 15);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t q = wide_block() * (LP_THREADS / 64) + wave;
+    if (q >= N) return; // whole wavefronts; no barrier below
+    // what the column needs is asked for at once: its word, the first round of its runs, its slices
+    const int64_t word = logp ? tok[q] : -1;
+    const int runs = (int)((V + LP_RUN - 1) / LP_RUN);
+    const float *column_runs = TOP ? run_max + q * run_pitch : nullptr;
+    float piece[LP_AHEAD][4];
+    if constexpr (TOP)
+#pragma unroll
+        for (int k = 0; k < LP_AHEAD; ++k) lp_runs(piece[k], column_runs, 256 * k + 4 * lane, runs);
     LpSums a = lp_empty<T>();
-    if (q < N)
-        for (int64_t i = tid >> 4; i < slices; i += THREADS / 16) {
-            const float *p = part + i * 3 * N + q;
-            a = lp_join<T>(a, LpSums{p[0], p[N], p[2 * N]});
+    for (int64_t i0 = 0; i0 < slices; i0 += 64 * 4) {
+        float4 p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t i = i0 + 64 * k + lane;
+            p[k] = i < slices ? part[q * slices + i] : make_float4(Logit<T>::lowest, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-    for (int step = 16; step < 64; step *= 2)
+        for (int k = 0; k < 4; ++k)
+            if (i0 + 64 * k < slices) a = lp_join<T>(a, LpSums{p[k].x, p[k].y, p[k].z});
+    }
+    const float x = word >= 0 && word < V ? Logit<T>::widen(L[word * ldl + q]) : 0.f;
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2)
         a = lp_join<T>(a, LpSums{__shfl_xor(a.m, step, 64), __shfl_xor(a.s, step, 64), __shfl_xor(a.t, step, 64)});
-    if (lane < 16) join[wave][lane] = a;
-    __syncthreads();
-    if (tid < 16) {
-        a = join[0][tid];
-        for (int w = 1; w < WAVES; ++w) a = lp_join<T>(a, join[w][tid]);
-        // the sum was taken at the rounded reference r: brought to the maximum itself
-        const float c = lp_factor<T>(a.m), r = a.m * c, log_s = __log2f(a.s), log_m = log_s - __builtin_fmaf(a.m, c, -r);
-        const float ln_s = LP_LN2 * log_m;
-        column[0][tid] = a.m;
-        column[1][tid] = ln_s;
-        if (q < N) {
-            const bool empty = a.s == 0.f; // every logit is -infinity
-            stats[q] = empty ? -__builtin_inff() : a.m;
-            stats[N + q] = log_m;
-            if (entropy) entropy[q] = empty ? 0.f : LP_LN2 * (log_s - a.t / a.s);
-            if (logp) {
-                const int64_t w = tok[q];
-                float v = 0.f;
-                if (w >= V) v = __builtin_nanf("");
-                else if (w >= 0) v = empty ? -__builtin_inff() : Logit<T>::widen(L[w * ldl + q]) - a.m - ln_s;
-                logp[q] = v;
-            }
-        }
+    // the sum was taken at the rounded reference r: brought to the maximum itself
+    const float c = lp_factor<T>(a.m), r = a.m * c, log_s = __log2f(a.s), log_m = log_s - __builtin_fmaf(a.m, c, -r);
+    const float ln_s = LP_LN2 * log_m;
+    if (lane == 0) {
+        const bool empty = a.s == 0.f; // every logit is -infinity
+        stats[q] = empty ? -__builtin_inff() : a.m;
+        stats[N + q] = log_m;
+        if (entropy) entropy[q] = empty ? 0.f : LP_LN2 * (log_s - a.t / a.s);
+        if (logp) logp[q] = word < 0 ? 0.f : word >= V ? __builtin_nanf("") : empty ? -__builtin_inff() : x - a.m - ln_s;
     }
     if constexpr (TOP) {
-        __shared__ LpList lists[WAVES];
-        __syncthreads();
-        const int64_t qw = q0 + wave;
-        if (qw >= N) return;
-        const int count = lp_top(lists[wave], L, ldl, V, N, qw, run_max, K, lane);
+        __shared__ LpList lists[LP_THREADS / 64];
+        LpList &l = lists[wave];
+        const int count = lp_top(l, L, ldl, (int)V, q, column_runs, run_more + q * run_pitch, runs, piece, K, lane);
         if (lane < K) {
-            top_ids[lane * N + qw] = lane < count ? lists[wave].word[lane] : -1;
-            top_logp[lane * N + qw] =
-                lane < count ? lists[wave].value[lane] - column[0][wave] - column[1][wave] : -__builtin_inff();
+            top_ids[lane * N + q] = lane < count ? lp_key_word(l.key[lane]) : -1;
+            top_logp[lane * N + q] = lane < count ? lp_key_logit(l.key[lane]) - a.m - ln_s : -__builtin_inff();
         }
     }
 }
 
-// dx_v = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy); a lane owns P columns and 16 rows.
+// dx_v = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy); a lane owns P columns and the `batches` batches of 8 rows from
+// ((block * ty_count) + ty) * batches on.
 template <typename T, int P>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N,
                                                                    const int64_t *__restrict__ tok, const float *__restrict__ stats,
                                                                    const float *__restrict__ entropy, const float *__restrict__ g_logp,
                                                                    const float *__restrict__ g_entropy, T *__restrict__ DL, int64_t lddl,
-                                                                   int tx_count, int ty_count, int64_t row_blocks)
+                                                                   int tx_count, int ty_count, int64_t col_blocks, int64_t batches)
 {
+    __shared__ float column[7][64 * P]; // factor, reference, log2 of the sum, the two gradients, entropy, word of every column
     const int tid = threadIdx.x;
     const int ty = tid / tx_count, tx = tid - ty * tx_count;
     const int64_t blk = wide_block();
-    const int64_t cb = blk / row_blocks, rb = blk - cb * row_blocks;
-    const int64_t q0 = (cb * tx_count + tx) * P, v0 = (rb * ty_count + ty) * LP_BATCH;
-    if (ty >= ty_count || q0 >= N || v0 >= V) return;
+    const int64_t rb = blk / col_blocks, cb = blk - rb * col_blocks; // neighbours read the same rows
+    const int64_t q0 = (cb * tx_count + tx) * P, first = (rb * ty_count + ty) * batches * LP_GRAD;
+    for (int e = tid; e < tx_count * P; e += blockDim.x) {
+        const int64_t q = cb * tx_count * P + e;
+        if (q >= N) break;
+        const float m = fmaxf(stats[q], Logit<T>::lowest), c = lp_factor<T>(m), r = m * c;
+        float log_s = stats[N + q] + __builtin_fmaf(m, c, -r);
+        const int64_t w = g_logp ? tok[q] : -1;
+        float gl = w < 0 ? 0.f : g_logp[q];
+        const float gh = g_entropy ? g_entropy[q] * LP_LN2 : 0.f; // log p below is in base 2
+        float h = g_entropy ? entropy[q] * LP_LOG2E : 0.f;
+        // Columns that hold a NaN or +infinity, and words that are none: NaN, through gl, since log p is cut below.
+        // No gradient comes in: none goes out, whatever the logits.  A column of -infinity alone: every p is 0.
+        const bool none = gl == 0.f && gh == 0.f;
+        if (!none && (w >= V || log_s != log_s)) gl = __builtin_nanf("");
+        if (none) h = 0.f;
+        if (none || log_s == -__builtin_inff()) log_s = 0.f;
+        column[0][e] = c;
+        column[1][e] = r;
+        column[2][e] = log_s;
+        column[3][e] = gl;
+        column[4][e] = gh;
+        column[5][e] = h;
+        column[6][e] = __builtin_bit_cast(float, w >= 0 && w < V ? (int)w : -1);
+    }
+    __syncthreads();
+    if (ty >= ty_count || q0 >= N || first >= V) return;
     float c[P], r[P], log_s[P], gl[P], gh[P], h[P];
-    int64_t word[P];
+    int word[P]; // from the lane's first row on
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int64_t q = q0 + p < N ? q0 + p : N - 1;
-        const float m = fmaxf(stats[q], Logit<T>::lowest);
-        c[p] = lp_factor<T>(m);
-        r[p] = m * c[p];
-        log_s[p] = stats[N + q] + __builtin_fmaf(m, c[p], -r[p]);
-        if (log_s[p] == -__builtin_inff()) log_s[p] = 0.f; // an empty column: every probability is 0
-        const int64_t w = g_logp ? tok[q] : -1;
-        gl[p] = w < 0 ? 0.f : w >= V ? __builtin_nanf("") : g_logp[q];
-        word[p] = w - v0;
-        gh[p] = g_entropy ? g_entropy[q] * LP_LN2 : 0.f; // log p below is in base 2
-        h[p] = g_entropy ? entropy[q] * LP_LOG2E : 0.f;
+        const int e = tx * P + p;
+        c[p] = column[0][e];
+        r[p] = column[1][e];
+        log_s[p] = column[2][e];
+        gl[p] = column[3][e];
+        gh[p] = column[4][e];
+        h[p] = column[5][e];
+        const int64_t w = __builtin_bit_cast(int, column[6][e]);
+        word[p] = w >= first && w < first + batches * LP_GRAD ? (int)(w - first) : -1;
     }
-    const int left = V - v0 < LP_BATCH ? (int)(V - v0) : LP_BATCH;
-    const T *src = L + v0 * ldl + q0;
-    T *dst = DL + v0 * lddl + q0;
-    Piece<T, P> x[LP_BATCH];
+    const auto batch = [&](int64_t v0, auto words) {
+        const int left = V - v0 < LP_GRAD ? (int)(V - v0) : LP_GRAD;
+        Piece<T, P> x[LP_GRAD];
+        lp_load<T, P, false, LP_GRAD>(x, L + v0 * ldl + q0, ldl, left);
+        T *dst = DL + v0 * lddl + q0;
 #pragma unroll
-    for (int i = 0; i < LP_BATCH; ++i) x[i] = *reinterpret_cast<const Piece<T, P> *>(src + (i < left ? i : left - 1) * ldl);
+        for (int i = 0; i < LP_GRAD; ++i) {
+            Piece<T, P> o;
 #pragma unroll
-    for (int i = 0; i < LP_BATCH; ++i) {
-        Piece<T, P> o;
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const float l = __builtin_fmaf(Logit<T>::widen(x[i].v[p]), c[p], -r[p]) - log_s[p], e = lp_exp2(l);
-            const float g = e * __builtin_fmaf(gh[p], lp_finite(l) + h[p], gl[p]);
-            const float v = (word[p] == i ? gl[p] : 0.f) - g;
-            o.v[p] = Logit<T>::narrow(gl[p] == 0.f && gh[p] == 0.f ? 0.f : v); // no gradient comes in: none goes out, whatever the logits
+            for (int p = 0; p < P; ++p) {
+                // (a NaN becomes -200)
+                const float l = __builtin_amdgcn_fmed3f(__builtin_fmaf(Logit<T>::widen(x[i].v[p]), c[p], -r[p]) - log_s[p], -200.f, 1.f);
+                float g = -lp_exp2(l) * __builtin_fmaf(gh[p], l + h[p], gl[p]);
+                if constexpr (decltype(words)::value) g += word[p] == (int)(v0 - first) + i ? gl[p] : 0.f;
+                o.v[p] = Logit<T>::narrow(g);
+            }
+            if (i < left) *reinterpret_cast<Piece<T, P> *>(dst + i * lddl) = o;
         }
-        if (i < left) *reinterpret_cast<Piece<T, P> *>(dst + i * lddl) = o;
+    };
+#pragma unroll 1
+    for (int64_t v0 = first; v0 < first + batches * LP_GRAD && v0 < V; v0 += LP_GRAD) {
+        bool here = false; // few batches hold one of the wavefront's words
+#pragma unroll
+        for (int p = 0; p < P; ++p) here = here || (word[p] >= 0 && word[p] / LP_GRAD == (int)(v0 - first) / LP_GRAD);
+        if (__any(here)) batch(v0, std::true_type{});
+        else batch(v0, std::false_type{});
     }
 }
 
 // Columns per lane and lanes per row.  A piece of P columns is one load: P divides N and the row pitch, the base is aligned to
 // it.  Wider pieces need fewer instructions a column, and fewer lanes: they are taken while every SIMD still gets two
-// wavefronts of lanes with one run of rows each.
+// wavefronts of lanes with `rows` rows each.
 struct LpShape {
     int p, tx, ty;
     int64_t col_blocks;
 };
-static LpShape lp_shape(int es, int64_t V, int64_t N, int64_t bits, int rows)
+static LpShape lp_shape(int es, int64_t V, int64_t N, int64_t bits, int rows, int most_bytes)
 {
     LpShape s;
     s.p = 1;
     const int64_t pieces_of_rows = (V + rows - 1) / rows;
-    for (int p = 16 / es; p > 1; p /= 2) {
+    for (int p = most_bytes / es; p > 1; p /= 2) {
         if (N % p != 0 || (bits & (p * es - 1)) != 0) continue;
         if (p > 2 && pieces_of_rows * (N / p) < 131072) continue;
         s.p = p;
         break;
     }
     const int64_t pieces = N / s.p;
+    // few lanes in all: workgroups of one wavefront, so that more compute units take part
+    const int threads = pieces_of_rows * pieces <= 16384 ? 64 : LP_THREADS;
     s.tx = pieces < 64 ? (int)pieces : 64;
-    s.ty = LP_THREADS / s.tx;
+    s.ty = threads / s.tx;
     s.col_blocks = (pieces + s.tx - 1) / s.tx;
     return s;
 }
 
-// rows of the pass kernel's grid; the workspace holds three numbers per slice and column, then the run maxima
+// Workgroups of the pass kernel; the workspace holds four numbers per column and slice, then two per column and run of the top words.
 struct LpPlan {
     LpShape shape;
-    int64_t runs, slices;
+    int64_t runs, slices, run_pitch;
     uint64_t part_bytes, bytes;
 };
 static LpPlan lp_plan(int es, int64_t V, int64_t N, int32_t top, int64_t bits)
 {
     LpPlan p;
-    p.shape = lp_shape(es, V, N, bits, LP_RUN);
+    p.shape = lp_shape(es, V, N, bits, LP_RUN, 8);
     const int64_t all = (V + LP_RUN - 1) / LP_RUN;
     // runs a lane: as many as leave 2048 workgroups, eight for each compute unit
-    int64_t groups = (all + p.shape.ty - 1) / p.shape.ty * p.shape.col_blocks;
+    const int64_t groups = (all + p.shape.ty - 1) / p.shape.ty * p.shape.col_blocks;
     p.runs = groups / 2048 > 1 ? groups / 2048 : 1;
     p.slices = (all + p.runs * p.shape.ty - 1) / (p.runs * p.shape.ty);
-    p.part_bytes = (uint64_t)p.slices * 3 * (uint64_t)N * 4;
-    p.bytes = p.part_bytes + (top > 0 ? (uint64_t)all * (uint64_t)N * 4 : 0);
+    p.run_pitch = (all + 3) / 4 * 4;
+    p.part_bytes = (uint64_t)p.slices * 16 * (uint64_t)N;
+    p.bytes = p.part_bytes + (top > 0 ? (uint64_t)p.run_pitch * (uint64_t)N * 8 : 0);
     return p;
 }
 uint64_t logprobs_workspace_bytes(int es, int64_t V, int64_t N, int32_t top)
@@ -466,27 +628,39 @@ static int launch_logprobs_t(const T *L, int64_t ldl, int64_t V, int64_t N, cons
                              float *stats, int32_t top, int64_t *top_ids, float *top_logp, void *ws, hipStream_t stream)
 {
     const LpPlan p = lp_plan((int)sizeof(T), V, N, top, (int64_t)(uintptr_t)L | ldl * (int64_t)sizeof(T));
-    float *part = (float *)ws, *run_max = top > 0 ? (float *)((char *)ws + p.part_bytes) : nullptr;
-    const int64_t blocks = p.shape.col_blocks * p.slices, finish = (N + 15) / 16;
-    if (blocks > 0x7FFFFFFF || finish > 0x7FFFFFFF / 1024) return LRBI_ERR_SHAPE;
-#define LRBI_PASS(P)                                                                                                     \
-    LRBI_LAUNCH((logprobs_pass_kernel<T, P>), wide_grid(blocks, LP_THREADS), dim3(LP_THREADS), 0, stream, L, ldl, V, N, p.shape.tx, \
-                p.shape.ty, p.runs, p.slices, part, run_max)
+    float4 *part = (float4 *)ws;
+    float *run_max = (float *)((char *)ws + p.part_bytes);
+    uint32_t *run_more = (uint32_t *)run_max + p.run_pitch * N;
+    const int threads = p.shape.tx * p.shape.ty <= 64 ? 64 : LP_THREADS, per = LP_THREADS / 64;
+    const int64_t blocks = p.shape.col_blocks * p.slices, finish = (N + per - 1) / per;
+    if (blocks > 0x7FFFFFFF || finish > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
+    const bool column = N == 1 && ldl == 1 && ((uintptr_t)L & 15) == 0;
+#define LRBI_PASS_TOP(P, COLUMN, TOP)                                                                                               \
+    LRBI_LAUNCH((logprobs_pass_kernel<T, P, COLUMN, TOP>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N, p.shape.tx, \
+                p.shape.ty, p.shape.col_blocks, p.runs, p.slices, part, run_max, run_more, p.run_pitch)
+#define LRBI_PASS(P, COLUMN)                                                                                               \
+    do {                                                                                                                   \
+        if (top > 0) LRBI_PASS_TOP(P, COLUMN, true);                                                                       \
+        else LRBI_PASS_TOP(P, COLUMN, false);                                                                              \
+    } while (0)
     switch (p.shape.p) {
-    case 1: LRBI_PASS(1); break;
-    case 2: LRBI_PASS(2); break;
-    case 4: LRBI_PASS(4); break;
+    case 1:
+        if (column) LRBI_PASS(1, true);
+        else LRBI_PASS(1, false);
+        break;
+    case 2: LRBI_PASS(2, false); break;
     default:
-        if constexpr (sizeof(T) == 2) LRBI_PASS(8);
+        if constexpr (sizeof(T) == 2) LRBI_PASS(4, false);
         break;
     }
 #undef LRBI_PASS
-    if (top > 0)
-        LRBI_LAUNCH((logprobs_finish_kernel<T, true>), dim3((unsigned)finish), dim3(1024), 0, stream, L, ldl, V, N, tok, part, p.slices,
-                    run_max, logp, entropy, stats, top, top_ids, top_logp);
-    else
-        LRBI_LAUNCH((logprobs_finish_kernel<T, false>), dim3((unsigned)finish), dim3(256), 0, stream, L, ldl, V, N, tok, part, p.slices,
-                    run_max, logp, entropy, stats, top, top_ids, top_logp);
+#undef LRBI_PASS_TOP
+#define LRBI_FINISH(TOP)                                                                                                   \
+    LRBI_LAUNCH((logprobs_finish_kernel<T, TOP>), wide_grid(finish, LP_THREADS), dim3(LP_THREADS), 0, stream, L, ldl, V, N, tok, part,  \
+                p.slices, run_max, run_more, p.run_pitch, logp, entropy, stats, top, top_ids, top_logp)
+    if (top > 0) LRBI_FINISH(true);
+    else LRBI_FINISH(false);
+#undef LRBI_FINISH
     return LRBI_OK;
 }
 int launch_logprobs(lrbi_dtype dt, const void *dL, int64_t ldl, int64_t V, int64_t N, const int64_t *dTok, float *dLogp, float *dEntropy,
@@ -507,12 +681,16 @@ static int launch_logprobs_grad_t(const T *L, int64_t ldl, int64_t V, int64_t N,
                                   hipStream_t stream)
 {
     const int64_t bits = (int64_t)((uintptr_t)L | (uintptr_t)DL) | (ldl | lddl) * (int64_t)sizeof(T);
-    const LpShape s = lp_shape((int)sizeof(T), V, N, bits, LP_BATCH);
-    const int64_t row_blocks = (V + (int64_t)s.ty * LP_BATCH - 1) / ((int64_t)s.ty * LP_BATCH), blocks = s.col_blocks * row_blocks;
+    const LpShape s = lp_shape((int)sizeof(T), V, N, bits, LP_GRAD, 16);
+    const int threads = s.tx * s.ty <= 64 ? 64 : LP_THREADS;
+    // batches a lane, for whose columns it reads 28 bytes each: up to eight while 2048 workgroups are left
+    int64_t batches = (V + LP_GRAD - 1) / LP_GRAD / s.ty * s.col_blocks / 2048;
+    batches = batches < 1 ? 1 : batches > 8 ? 8 : batches;
+    const int64_t rows = s.ty * batches * LP_GRAD, row_blocks = (V + rows - 1) / rows, blocks = s.col_blocks * row_blocks;
     if (blocks > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
 #define LRBI_GRAD(P)                                                                                                       \
-    LRBI_LAUNCH((logprobs_grad_kernel<T, P>), wide_grid(blocks, LP_THREADS), dim3(LP_THREADS), 0, stream, L, ldl, V, N, tok, stats,  \
-                entropy, g_logp, g_entropy, DL, lddl, s.tx, s.ty, row_blocks)
+    LRBI_LAUNCH((logprobs_grad_kernel<T, P>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N, tok, stats, entropy,  \
+                g_logp, g_entropy, DL, lddl, s.tx, s.ty, s.col_blocks, batches)
     switch (s.p) {
     case 1: LRBI_GRAD(1); break;
     case 2: LRBI_GRAD(2); break;
