@@ -116,13 +116,18 @@ __global__ __launch_bounds__(256) void quant_unpack_kernel(const unsigned char *
     }
 }
 
-// Y = Wq X.  A workgroup owns 16 rows of W; its wavefronts take turns along the columns, 128 at a time: lane (row = lane % 16,
-// block = lane / 16) loads the 16 bytes of one block and its scale, and the four products of 16 x 16 x 32 that follow take
-// eight codes of every block each (the order of a sum's terms is free as long as both operands have the same one).
-// X goes through LDS as [eight rows][column], the eight rows of a column 16 bytes, which is the other operand as it is read.
-// fp32 X is split into three bf16 columns, x = x1 + x2 + x3 exactly, whose products are added in the end.
+// Y = Wq X.  The codes are read once, straight into registers, and that is what takes the time: 16384 x 16384, one column,
+// 142 MB.  A wavefront owns 16 rows of W and takes 512 of their columns at a time, the next 512 under way while it multiplies:
+// lane (row = lane % 16, block = lane / 16) loads the 16 bytes of one block of each 128 columns, and one piece of 16 scale
+// bytes for all of them.  The four products of 16 x 16 x 32 for 128 columns take eight codes of every block each (the order of
+// a sum's terms is free as long as both operands have the same one).  X goes through LDS as [eight rows][column], the eight
+// rows of a column 16 bytes, which is the other operand as it is read.  fp32 X is split into three bf16 columns, x = x1 + x2 +
+// x3 exactly, whose products are added in the end.
+// Of a workgroup's eight wavefronts WR own different rows (they share X: for many columns, whose X is what a workgroup reads
+// most of), the others every 8 / WR-th piece of 512 columns, their sums are added in LDS.
 static constexpr int QM_WAVES = 8;
-static constexpr int QM_CHUNK = 2048; // columns of W whose X is in LDS at a time
+static constexpr int QM_QUAD = 512; // columns of W a wavefront takes at a time: four times four blocks
+static constexpr int QM_LDS = 64 * 1024; // for X
 
 template <typename T> struct QmOperand {
     typedef T type;
@@ -159,87 +164,165 @@ __device__ __forceinline__ uint16_t qm_part(float x, int part)
     return (uint16_t)(u >> 16);
 }
 
-// NT: tiles of 16 operand columns.  cols: columns of X that this launch's workgroups take at a time.
-template <typename T, int NT>
+struct QmQuad { // a lane's share of 512 columns
+    uint4 codes[4];
+    uint32_t scales[4];
+};
+struct alignas(4) QmScales {
+    uint32_t v[4];
+};
+// columns from 512 quad on; what lies behind the last block is read from it (X is zero there) at a scale of 1
+__device__ __forceinline__ void qm_load(QmQuad &w, const unsigned char *crow, const unsigned char *srow, int64_t quad, int64_t blocks, int blkq)
+{
+    const int64_t b0 = quad * 16;
+    if (b0 + 16 <= blocks) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) w.codes[g] = *reinterpret_cast<const uint4 *>(crow + (b0 + 4 * g + blkq) * 16);
+        const QmScales s = *reinterpret_cast<const QmScales *>(srow + b0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) w.scales[g] = s.v[g] >> (8 * blkq);
+    } else {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int64_t b = b0 + 4 * g + blkq, in = b < blocks ? b : blocks - 1;
+            w.codes[g] = *reinterpret_cast<const uint4 *>(crow + in * 16);
+            w.scales[g] = b < blocks ? srow[b] : (uint32_t)STORE_BIAS;
+        }
+    }
+}
+
+// NT: tiles of 16 operand columns.  cols: columns of X that a workgroup takes at a time; chunk: columns of W whose X is in LDS at a
+// time, a multiple of 512 (8 / WR).  VX: columns of X that are loaded together (they divide cols and N and are aligned); 0: a
+// single column, contiguous and 16-byte aligned.
+template <typename T, int NT, int WR, int VX>
 __global__ __launch_bounds__(64 * QM_WAVES) void quant_matvec_kernel(const unsigned char *__restrict__ codes, int64_t ldc,
                                                                      const unsigned char *__restrict__ scales, int64_t lds, int64_t m,
                                                                      int64_t n, const T *__restrict__ X, int64_t ldx, int64_t N, int cols,
-                                                                     T *__restrict__ Y, int64_t ldy, int64_t row_blocks)
+                                                                     int chunk, T *__restrict__ Y, int64_t ldy, int64_t row_blocks, int64_t workgroups)
 {
     typedef typename QmOperand<T>::type Op;
-    constexpr int PARTS = QmOperand<T>::parts;
+    constexpr int PARTS = QmOperand<T>::parts, WK = QM_WAVES / WR;
     extern __shared__ uint4 lrbi_dyn_smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % WK, wr = wave / WK;
     const int64_t blk = wide_block();
-    const int64_t cb = blk / row_blocks, rb = blk - cb * row_blocks;
-    const int64_t q0 = cb * cols, i0 = rb * 16;
+    const int64_t cb = blk / workgroups;
+    int64_t rb = blk - cb * workgroups;
+    const int64_t q0 = cb * cols;
     if (q0 >= N) return;
     const int nc = N - q0 < cols ? (int)(N - q0) : cols; // columns of X here
     const int ops = nc * PARTS;                          // operand columns
-    uint16_t *Xs = (uint16_t *)lrbi_dyn_smem;            // [QM_CHUNK / 8][ops][8]
+    uint4 *Xs = lrbi_dyn_smem;                           // [chunk / 8][ops]
+    float *red = (float *)(Xs + chunk / 8 * ops);        // [two in turn][wave][tile][16 rows][16 columns + 1]
     const int r = lane & 15, blkq = lane >> 4;
-    const int64_t row = i0 + r < m ? i0 + r : m - 1;
-    const int64_t blocks = (n + STORE_BLOCK - 1) / STORE_BLOCK;
-    const unsigned char *crow = codes + row * ldc, *srow = scales + row * lds;
+    const int64_t blocks = (n + STORE_BLOCK - 1) / STORE_BLOCK, quads = (n + QM_QUAD - 1) / QM_QUAD;
+    const unsigned char *crow = nullptr, *srow = nullptr;
     int opc[NT]; // this lane's operand column of each tile (past the last one: any)
 #pragma unroll
     for (int t = 0; t < NT; ++t) opc[t] = 16 * t + r < ops ? 16 * t + r : ops - 1;
+
+    QmQuad w, next;
+    const bool once = chunk >= n; // all of X stays in LDS
+    const int64_t rounds = (quads + WK - 1) / WK;
+    int64_t turn = 0;
+    auto begin = [&](int64_t block) __attribute__((always_inline)) { // asks for the first columns of a block of rows
+        const int64_t i = block * (16 * WR) + 16 * wr + r, row = i < m ? i : m - 1;
+        crow = codes + row * ldc;
+        srow = scales + row * lds;
+        // Rows a power of two apart have the same columns in the same memory channels: where all of X is there, each block of rows
+        // begins at another of its rounds.
+        turn = once ? block % rounds : 0;
+        if (turn * WK + wk < quads) qm_load(next, crow, srow, turn * WK + wk, blocks, blkq);
+    };
+    begin(rb);
+    int half = 0;
+    for (; rb < row_blocks; rb += workgroups, half ^= 1) {
+    const int64_t i0 = rb * (16 * WR);
     f32x4 acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    for (int64_t k0 = 0; k0 < n; k0 += QM_CHUNK) {
-        const int64_t k1 = (k0 + QM_CHUNK < blocks * STORE_BLOCK ? k0 + QM_CHUNK : blocks * STORE_BLOCK);
-        const int kk = (int)(k1 - k0); // a multiple of 32
-        if (k0) __syncthreads();
-        for (int e = tid; e < kk * nc; e += 64 * QM_WAVES) {
-            const int j = e / nc, c = e - j * nc;
-            const T x = k0 + j < n ? X[(k0 + j) * ldx + q0 + c] : T{};
+    int64_t done = 0; // rounds
+    for (int64_t k0 = 0; k0 < n; k0 += chunk) {
+        const int kk = (int)(k0 + chunk < quads * QM_QUAD ? chunk : quads * QM_QUAD - k0); // a multiple of 512
+        constexpr int V = VX ? VX : 1; // eight rows of V columns a lane
+        const int per_row = nc / V;
+        const bool fill = !once || rb == blk - cb * workgroups;
+        if (!once) __syncthreads(); // the last chunk has been read
+        for (int e = fill ? tid : kk; e < kk / 8 * per_row; e += 64 * QM_WAVES) {
+            const int j8 = e / per_row, c = (e - j8 * per_row) * V;
+            const int64_t j = k0 + 8 * j8;
+            struct alignas(V * sizeof(T)) Row {
+                T v[V];
+            } x[8];
+            if (VX == 0 && j + 8 <= n) {
+                uint4 v[sizeof(T) / 2];
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) Xs[((j >> 3) * ops + c * PARTS + p) * 8 + (j & 7)] = qm_part(x, p);
+                for (int k = 0; k < (int)sizeof(T) / 2; ++k) v[k] = reinterpret_cast<const uint4 *>(X + j)[k];
+                __builtin_memcpy(x, v, sizeof(v));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (j + k < n) x[k] = *reinterpret_cast<const Row *>(X + (j + k) * ldx + q0 + c);
+                    else x[k] = Row{};
+                }
+            }
+#pragma unroll
+            for (int l = 0; l < V; ++l)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    uint16_t h[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) h[k] = qm_part(x[k].v[l], p);
+                    uint4 v;
+                    __builtin_memcpy(&v, h, 16);
+                    Xs[j8 * ops + (c + l) * PARTS + p] = v;
+                }
         }
-        __syncthreads();
-        for (int64_t b0 = k0 / STORE_BLOCK + 4 * wave; b0 < k1 / STORE_BLOCK; b0 += 4 * QM_WAVES) {
-            const int64_t b = b0 + blkq;
-            const bool in = b < k1 / STORE_BLOCK;
-            const int64_t bc = in ? b : b0;
-            uint4 w = *reinterpret_cast<const uint4 *>(crow + bc * 16);
-            const float s = scale_operand(srow[bc]);
-            if (!in) w = make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-            const uint16_t *xb = Xs + (int64_t)(bc - k0 / STORE_BLOCK) * 4 * ops * 8;
+        if (fill) __syncthreads();
+        for (const int64_t end = once ? rounds : (k0 + kk + WK * QM_QUAD - 1) / (WK * QM_QUAD); done < end; ++done) {
+            const int64_t quad = turn * WK + wk;
+            if (++turn == rounds) turn = 0;
+            w = next;
+            if (done + 1 < rounds && turn * WK + wk < quads) qm_load(next, crow, srow, turn * WK + wk, blocks, blkq);
+            if (quad >= quads) continue;
+            const uint4 *xb = Xs + (quad * 64 - k0 / 8 + 4 * blkq) * ops;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const q_u32x4 a = {widen4<0>(Op{}, ws[i], s), widen4<1>(Op{}, ws[i], s), widen4<2>(Op{}, ws[i], s),
-                                   widen4<3>(Op{}, ws[i], s)};
+            for (int g = 0; g < 4; ++g) {
+                const float s = scale_operand(w.scales[g] & 255u);
+                const uint32_t ws[4] = {w.codes[g].x, w.codes[g].y, w.codes[g].z, w.codes[g].w};
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    q_u32x4 x = *reinterpret_cast<const q_u32x4 *>(xb + (i * ops + opc[t]) * 8);
-                    if (!in) x = q_u32x4{0u, 0u, 0u, 0u}; // (an infinity in it times the zero codes would be NaN)
-                    acc[t] = mfma_16x16x32(Op{}, a, x, acc[t]);
+                for (int k = 0; k < 4; ++k) {
+                    const q_u32x4 a = {widen4<0>(Op{}, ws[k], s), widen4<1>(Op{}, ws[k], s), widen4<2>(Op{}, ws[k], s),
+                                       widen4<3>(Op{}, ws[k], s)};
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        acc[t] = mfma_16x16x32(Op{}, a, *reinterpret_cast<const q_u32x4 *>(xb + (16 * g + k) * ops + opc[t]), acc[t]);
                 }
             }
         }
     }
-    // the wavefronts' sums, in their order
-    __syncthreads();
-    float *red = (float *)lrbi_dyn_smem; // [wave][tile][16 rows][16 columns + 1]
+    if (rb + workgroups < row_blocks) begin(rb + workgroups);
+    // the wavefronts' sums, in their order (the other half is written next: what is read here is not overwritten before the
+    // barrier after that)
+    float *part = red + half * (QM_WAVES * NT * 16 * 17);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) red[((wave * NT + t) * 16 + 4 * blkq + v) * 17 + r] = acc[t][v];
+        for (int v = 0; v < 4; ++v) part[((wave * NT + t) * 16 + 4 * blkq + v) * 17 + r] = acc[t][v];
     __syncthreads();
-    for (int e = tid; e < 16 * nc; e += 64 * QM_WAVES) {
-        const int i = e / nc, c = e - i * nc;
+    for (int e = tid; e < 16 * WR * nc; e += 64 * QM_WAVES) {
+        const int il = e / nc, c = e - il * nc;
         float y = 0.f;
 #pragma unroll
         for (int p = PARTS - 1; p >= 0; --p) { // the small parts first
             const int op = c * PARTS + p;
-            float part = 0.f;
-            for (int w = 0; w < QM_WAVES; ++w) part += red[((w * NT + (op >> 4)) * 16 + i) * 17 + (op & 15)];
-            y += part;
+            float sum = 0.f;
+#pragma unroll
+            for (int v = 0; v < WK; ++v) sum += part[((((il >> 4) * WK + v) * NT + (op >> 4)) * 16 + (il & 15)) * 17 + (op & 15)];
+            y += sum;
         }
-        if (i0 + i < m) qm_store(Y + (i0 + i) * ldy + q0 + c, y);
+        if (i0 + il < m) qm_store(Y + (i0 + il) * ldy + q0 + c, y);
+    }
     }
 }
 
@@ -294,13 +377,35 @@ static int launch_matvec_t(const unsigned char *codes, int64_t ldc, const unsign
     constexpr int PARTS = QmOperand<T>::parts;
     const int nt = N * PARTS <= 16 ? 1 : 2;
     const int most = 16 * nt / PARTS, cols = N < most ? (int)N : most;
-    const int64_t row_blocks = (m + 15) / 16, groups = row_blocks * ((N + cols - 1) / cols);
+    const int64_t bits = (int64_t)(uintptr_t)X | ldx * (int64_t)sizeof(T);
+    const bool column = N == 1 && ldx == 1 && ((uintptr_t)X & 15) == 0;
+    const bool fours = N % 4 == 0 && cols % 4 == 0 && (bits & (4 * sizeof(T) - 1)) == 0;
+    // Wavefronts on different rows share X in LDS and add up fewer sums; there are fewer workgroups.  As many as leave one for
+    // every compute unit (us, with 1, 2, 4: 8192 x 8192, 7 columns f16 28 / 22 / 25; 16384 x 4096, 8 columns 20 / 14.5 / 12;
+    // 2000 x 4000, 3 columns 8.6 / 8.5 / 10), two for more than 8 operand columns, whose X fills LDS (6000 x 3000, 20 columns 13 / 10 /
+    // 12); one 16-bit column is little to share (300 x 16384 9.7 / 14 / 22, 16384 x 16384 34.8 / 38.6 / 34.5).
+    int wr = m >= 64 * 256 ? 4 : m >= 32 * 256 || cols * PARTS > 8 ? 2 : 1;
+    if (column && sizeof(T) == 2) wr = 1;
+    const int64_t row_blocks = (m + 16 * wr - 1) / (16 * wr), col_blocks = (N + cols - 1) / cols;
+    // X of a chunk in LDS: all of it where it fits, otherwise whole rounds of the wavefronts
+    const int64_t round = (int64_t)QM_QUAD * (QM_WAVES / wr), per_row = (int64_t)cols * PARTS * 2, all = (n + QM_QUAD - 1) / QM_QUAD * QM_QUAD;
+    int64_t chunk = QM_LDS / per_row / round * round;
+    if (chunk < round) chunk = round;
+    if (chunk > all) chunk = all;
+    // workgroups that keep X take several blocks of rows: two on a compute unit
+    const int64_t workgroups = chunk == all && row_blocks > 512 ? 512 : row_blocks, groups = workgroups * col_blocks;
     if (groups > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    const size_t xs = (size_t)QM_CHUNK * cols * PARTS * 2, red = (size_t)QM_WAVES * nt * 16 * 17 * 4, smem = xs > red ? xs : red;
-    auto kern = nt == 1 ? quant_matvec_kernel<T, 1> : quant_matvec_kernel<T, 2>;
+    const size_t smem = (size_t)(chunk * per_row) + (size_t)2 * QM_WAVES * nt * 16 * 17 * 4;
+#define LRBI_QM(NT, WR) (fours ? quant_matvec_kernel<T, NT, WR, 4> : quant_matvec_kernel<T, NT, WR, 1>)
+    auto kern = nt == 2   ? (wr == 4 ? LRBI_QM(2, 4) : LRBI_QM(2, 2))
+                : !column ? (wr == 4 ? LRBI_QM(1, 4) : wr == 2 ? LRBI_QM(1, 2) : LRBI_QM(1, 1))
+                          : quant_matvec_kernel<T, 1, 1, 0>;
+#undef LRBI_QM
+    if constexpr (sizeof(T) == 4)
+        if (column && wr > 1) kern = wr == 4 ? quant_matvec_kernel<T, 1, 4, 0> : quant_matvec_kernel<T, 1, 2, 0>;
     LRBI_SET_MAX_LDS(kern, smem);
-    LRBI_LAUNCH(kern, wide_grid(groups, 64 * QM_WAVES), dim3(64 * QM_WAVES), smem, stream, codes, ldc, scales, lds, m, n, X, ldx, N, cols, Y,
-                ldy, row_blocks);
+    LRBI_LAUNCH(kern, wide_grid(groups, 64 * QM_WAVES), dim3(64 * QM_WAVES), smem, stream, codes, ldc, scales, lds, m, n, X, ldx, N, cols,
+                (int)chunk, Y, ldy, row_blocks, workgroups);
     return LRBI_OK;
 }
 int launch_quant_matvec(lrbi_dtype dt, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m, int64_t n,
