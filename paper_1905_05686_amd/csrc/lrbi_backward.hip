@@ -499,6 +499,12 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
         if (row < rows) {
             if (VEC) {
                 if (qq < N) v = *reinterpret_cast<const uint4 *>(base + row * ld + qq); // N % 8 == 0
+            } else if (CODES && qq + 8 <= N) { // 16 bytes at any element's address
+                struct __attribute__((packed, aligned(2))) Unaligned {
+                    uint32_t x, y, z, w;
+                };
+                const Unaligned u = *reinterpret_cast<const Unaligned *>(base + row * ld + qq);
+                v = make_uint4(u.x, u.y, u.z, u.w);
             } else {
                 uint16_t tmp[8];
 #pragma unroll
@@ -598,7 +604,8 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
     // 64 columns may lie in the next tile column; words 2 and 3 of the I_z rows and a second set of I_p words (behind
     // the first one: one word per row) then come from that tile.
     const bool half = (g.c % BJ) != 0 && (g.c % 64) == 0 && g.k <= 32;
-    const bool lined_up = ((g.c % BJ) == 0 || half) && (g.r % BI) == 0 && g.k <= FAST_MAX_K && !g.ragged;
+    // (a tile that the matrix cuts off has whole factors all the same, and what lies outside is not stored)
+    const bool lined_up = ((g.c % BJ) == 0 || half) && (g.r % BI) == 0 && g.k <= FAST_MAX_K && (CODES || !g.ragged);
     if (lined_up) {
         const int ti = (int)(i0 / g.r), tj = j0 / g.c;
         const int il0 = (int)(i0 - (int64_t)ti * g.r), coff = j0 - tj * g.c;
@@ -829,8 +836,8 @@ int launch_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, con
                 int64_t ldxs, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
 {
     if (dt == LRBI_F32) return launch_f32_grad(g, (const float *)dDY, lddy, dX, ldx, dXScales, ldxs, N, dIp, dIz, (float *)dDW, lddw, stream);
-    if (!dXScales && grad256_wins(g, N) && grad256_ok(g, dDY, lddy, dX, ldx, N))
-        return launch_grad256(g, dt, dDY, lddy, dX, ldx, N, dIp, dIz, dDW, lddw, stream);
+    if (grad256_wins(g, N) && grad256_ok(g, dDY, lddy, dX, ldx, N))
+        return launch_grad256(g, dt, dDY, lddy, dX, ldx, dXScales, ldxs, N, dIp, dIz, dDW, lddw, stream);
     const int64_t iblocks = (g.m + 127) / 128, jblocks = (g.n + BJ - 1) / BJ;
     const int64_t blocks = iblocks * jblocks;
     if (blocks > 0x7FFFFFFF) return LRBI_ERR_SHAPE;

@@ -10,9 +10,14 @@
 // The mask touches only the output: its bits under the tile are formed once (Eq. 3), in the first iteration, from factor
 // slices in LDS (tiles line up with 64 columns and 128 rows), and select on the way out.
 // 4096 x 4096 bf16, 512 x 512 tiles: batch 1024 51 -> 39 us, 512 33 -> 27, 256 24 -> 21.
+//
+// From an activation checkpoint (8-bit codes, a scale per 32 batch columns: one slab) X is staged as it is stored, 8 KB a slab, and
+// widened between the LDS read and the products, four instructions for the eight codes of two matrix instructions.  The scale
+// bytes of eight slabs at a time go to LDS the same way, two sets in turn.
 #include "lrbi_internal.hpp"
 #include "lrbi_lds_dma.hpp"
 #include "lrbi_mfma_common.hpp"
+#include "lrbi_store.hpp"
 
 namespace lrbi {
 
@@ -27,22 +32,38 @@ static constexpr int G256_HU = G256_B / 64;
 static constexpr int G256_FZ_ROW = G256_HU * 8;
 static constexpr int G256_FZ_SET = FAST_MAX_K * G256_FZ_ROW;
 
-struct SmemG256 {
-    static constexpr size_t mt_off = (size_t)G256_NS * G256_STAGE;
+template <bool CODES> struct SmemG256 {
+    static constexpr int stage = CODES ? G256_STAGE_X + 8192 : G256_STAGE; // dY, then X: 256 rows x 64 bytes, or 32 of codes
+    static constexpr size_t mt_off = (size_t)G256_NS * stage;
     static constexpr size_t fz_off = mt_off + G256_B * G256_MT_ROW;
     static constexpr size_t fip_off = fz_off + 2 * G256_FZ_SET;
-    static constexpr size_t bytes = fip_off + G256_B * G256_HU * 2 * 4;
+    static constexpr size_t sc_off = fip_off + G256_B * G256_HU * 2 * 4; // [2][256 rows][8 scale bytes]
+    static constexpr size_t bytes = sc_off + (CODES ? 2 * G256_B * 8 : 0);
 };
-static_assert(SmemG256::bytes <= 160 * 1024, "LDS of a compute unit");
+static_assert(SmemG256<false>::bytes <= 160 * 1024, "LDS of a compute unit");
 
-template <typename Tag>
+__device__ __forceinline__ u32x4 g256_widen(F16Tag, u32x2 w, uint32_t s)
+{
+    const uint4 v = widen8_f16(make_uint2(w.x, w.y), scale_operand(s));
+    return u32x4{v.x, v.y, v.z, v.w};
+}
+__device__ __forceinline__ u32x4 g256_widen(BF16Tag, u32x2 w, uint32_t s)
+{
+    const uint4 v = widen8_bf16(make_uint2(w.x, w.y), scale_operand(s));
+    return u32x4{v.x, v.y, v.z, v.w};
+}
+
+template <typename Tag, bool CODES>
 __global__ __launch_bounds__(G256_THREADS) LRBI_WAVES_PER_SIMD(2) void mfma_grad256_kernel(
-    Geom g, const uint16_t *__restrict__ DY, int64_t lddy, const uint16_t *__restrict__ X, int64_t ldx, int N,
+    Geom g, const uint16_t *__restrict__ DY, int64_t lddy, const std::conditional_t<CODES, unsigned char, uint16_t> *__restrict__ X,
+    int64_t ldx, const unsigned char *__restrict__ XS, int64_t ldxs, int N,
     const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz, uint16_t *__restrict__ DW, int64_t lddw, int iblocks,
     int jblocks, int xcd_remap, int w_vec_ok)
 {
     constexpr int NS = G256_NS;
-    using S = SmemG256;
+    using S = SmemG256<CODES>;
+    constexpr int STAGE = S::stage, PIECES = CODES ? 3 : 4; // load instructions of a wavefront per slab
+    constexpr int XB = CODES ? 1 : 2;                        // bytes of a value of X
     extern __shared__ uint4 lrbi_dyn_smem[];
     unsigned char *smem = (unsigned char *)lrbi_dyn_smem;
     unsigned char *Mt = smem + S::mt_off;            // [256][MT_ROW]     mask bytes of the tile
@@ -78,17 +99,29 @@ __global__ __launch_bounds__(G256_THREADS) LRBI_WAVES_PER_SIMD(2) void mfma_grad
         const int row = (wave + 8 * i) * 16 + (lane >> 2);
         const int p = (lane & 3) ^ ((row >> 2) & 3);
         avo[i] = (uint32_t)(((row < a_last ? row : a_last) * lddy + p * 8) * 2);
-        bvo[i] = (uint32_t)(((row < b_last ? row : b_last) * ldx + p * 8) * 2);
+        if constexpr (!CODES) bvo[i] = (uint32_t)(((row < b_last ? row : b_last) * ldx + p * 8) * 2);
     }
-    const uint16_t *aptr = DY + i0 * lddy, *bptr = X + (int64_t)j0 * ldx;
+    if constexpr (CODES) { // rows of 32 bytes, piece p of row q at slot p ^ ((q >> 3) & 1); wavefront w issues 32 rows
+        const int row = wave * 32 + (lane >> 1);
+        bvo[0] = (uint32_t)((row < b_last ? row : b_last) * ldx + ((lane & 1) ^ ((row >> 3) & 1)) * 16);
+    }
+    const uint16_t *aptr = DY + i0 * lddy;
+    const auto *bptr = X + (int64_t)j0 * ldx;
+    // scale bytes of slabs 8 t .. + 7: wavefront w asks for those of its 32 rows, two words a row (past the last slab: the last word)
+    const unsigned char *sptr = XS + (int64_t)j0 * ldxs;
+    const auto issue_scales = [&](int t) {
+        const int row = wave * 32 + (lane >> 1), word = 2 * t + (lane & 1), most = last >> 2;
+        load_to_lds4(lds_address(smem) + (uint32_t)(S::sc_off + (t & 1) * (G256_B * 8) + wave * 256), sptr,
+                     (uint32_t)((row < b_last ? row : b_last) * ldxs + (word < most ? word : most) * 4));
+    };
     int asl = 0, bsl = 0; // the slabs that are asked for next; past the last one it is fetched again
     const uint32_t lds0 = lds_address(smem);
     const uint32_t lds_w = lds0 + (uint32_t)wave * 1024u;
     auto issue_piece = [&](int stage, auto i_c) { // 0, 1: chunks of dY, 2, 3: of X; the second one moves on
         constexpr int i = decltype(i_c)::value;
-        const uint32_t sb = lds_w + (uint32_t)stage * G256_STAGE;
+        const uint32_t sb = lds_w + (uint32_t)stage * STAGE;
         if constexpr (i < 2) load_to_lds16(sb + i * 8192u, aptr, avo[i]);
-        else load_to_lds16(sb + G256_STAGE_X + (i - 2) * 8192u, bptr, bvo[i - 2]);
+        else if constexpr (i == 2 || !CODES) load_to_lds16(sb + G256_STAGE_X + (i - 2) * 8192u, bptr, bvo[i - 2]);
         if constexpr (i == 1) {
             if (asl < last) aptr += G256_BK;
             ++asl;
@@ -108,18 +141,29 @@ __global__ __launch_bounds__(G256_THREADS) LRBI_WAVES_PER_SIMD(2) void mfma_grad
             const uint32_t p = (uint32_t)(((2 * j + lg) ^ c3) * 16);
             afa[0][j] = (uint32_t)((wm * 64 + l32) * 64) + p;
             bfa[0][j] = (uint32_t)(G256_STAGE_X + (wn * 128 + l32) * 64) + p;
-            afa[1][j] = afa[0][j] + 2 * G256_STAGE;
-            bfa[1][j] = bfa[0][j] + 2 * G256_STAGE;
+            if constexpr (CODES) bfa[0][j] = (uint32_t)(G256_STAGE_X + (wn * 128 + l32) * 32 + (j ^ ((l32 >> 3) & 1)) * 16 + lg * 8);
+            afa[1][j] = afa[0][j] + 2 * STAGE;
+            bfa[1][j] = bfa[0][j] + 2 * STAGE;
         }
     }
-    u32x4 af[2][2], bf[2][4]; // [step][block]
+    std::conditional_t<CODES, u32x2, u32x4> bf[2][4]; // [step][block]
+    u32x4 af[2][2];
+    uint32_t scales[2][4]; // scale bytes of this and of the next four slabs
     auto read_a = [&](auto st_c, auto j_c, auto b_c) {
         constexpr int st = decltype(st_c)::value, j = decltype(j_c)::value, b = decltype(b_c)::value;
-        af[j][b] = *reinterpret_cast<const u32x4 *>(smem + afa[st >> 1][j] + (st & 1) * G256_STAGE + b * 2048);
+        af[j][b] = *reinterpret_cast<const u32x4 *>(smem + afa[st >> 1][j] + (st & 1) * STAGE + b * 2048);
     };
     auto read_b = [&](auto st_c, auto j_c, auto a_c) {
         constexpr int st = decltype(st_c)::value, j = decltype(j_c)::value, a = decltype(a_c)::value;
-        bf[j][a] = *reinterpret_cast<const u32x4 *>(smem + bfa[st >> 1][j] + (st & 1) * G256_STAGE + a * 2048);
+        bf[j][a] = *reinterpret_cast<const std::remove_reference_t<decltype(bf[j][a])> *>(smem + bfa[st >> 1][j] + (st & 1) * STAGE +
+                                                                                         a * (XB * 1024));
+    };
+    auto read_scales = [&](auto set_c, int s) { // of slabs s .. s + 3, a multiple of 4
+        constexpr int set = decltype(set_c)::value;
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+            scales[set][a] = *reinterpret_cast<const uint32_t *>(smem + S::sc_off + ((s >> 3) & 1) * (G256_B * 8) +
+                                                             (wn * 128 + a * 32 + l32) * 8 + (s & 4));
     };
     f32x16 acc[4][2];
 #pragma unroll
@@ -128,9 +172,15 @@ __global__ __launch_bounds__(G256_THREADS) LRBI_WAVES_PER_SIMD(2) void mfma_grad
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
-    auto mma = [&](auto j_c, auto a_c, auto b_c) {
-        constexpr int j = decltype(j_c)::value, a = decltype(a_c)::value, b = decltype(b_c)::value;
-        acc[a][b] = mfma_32x32x16(Tag{}, bf[j][a], af[j][b], acc[a][b]);
+    u32x4 wide; // codes of the current block, widened
+    auto mma = [&](auto j_c, auto a_c, auto b_c, auto st_c) {
+        constexpr int j = decltype(j_c)::value, a = decltype(a_c)::value, b = decltype(b_c)::value, st = decltype(st_c)::value;
+        if constexpr (CODES) {
+            if constexpr (b == 0) wide = g256_widen(Tag{}, bf[j][a], (scales[0][a] >> (8 * st)) & 255u);
+            acc[a][b] = mfma_32x32x16(Tag{}, wide, af[j][b], acc[a][b]);
+        } else {
+            acc[a][b] = mfma_32x32x16(Tag{}, bf[j][a], af[j][b], acc[a][b]);
+        }
     };
 
     using I0 = std::integral_constant<int, 0>;
@@ -172,7 +222,8 @@ __global__ __launch_bounds__(G256_THREADS) LRBI_WAVES_PER_SIMD(2) void mfma_grad
             load_to_lds4(lds0 + (uint32_t)(S::fip_off + q * 256), Ip, (uint32_t)(((t * g.r + il) * g.ipw + iw) * 4));
         }
     }
-    constexpr int kProloguePieces = (NS - 2) * 4 + 2;
+    if constexpr (CODES) issue_scales(0);
+    constexpr int kProloguePieces = (NS - 2) * PIECES + 2;
     static_for<NS - 1>([&](auto sc) {
         constexpr int st = decltype(sc)::value;
         issue_piece(st, I0{});
@@ -182,10 +233,11 @@ __global__ __launch_bounds__(G256_THREADS) LRBI_WAVES_PER_SIMD(2) void mfma_grad
             issue_piece(st, I3{});
         }
     });
-    wait_loads<kProloguePieces - 4>(); // slab 0
+    wait_loads<kProloguePieces - PIECES>(); // slab 0
     __syncthreads();
     static_for<2>([&](auto b) { read_a(I0{}, I0{}, b); });
     static_for<4>([&](auto a) { read_b(I0{}, I0{}, a); });
+    if constexpr (CODES) read_scales(I0{}, 0);
 
     // Eq. 3: a lane forms the four mask words of one row under 128 columns
     auto form_mask = [&]() {
@@ -221,30 +273,38 @@ __global__ __launch_bounds__(G256_THREADS) LRBI_WAVES_PER_SIMD(2) void mfma_grad
             constexpr int stn = (st + NS - 1) % NS; // stage of slab s + NS - 1
             constexpr int stp = (st + NS - 2) % NS; // stage of slab s + NS - 2
             if (s0 + st < nslabs) {
+                // the set that the last eight slabs have left; landed, and seen by all, long before it is read
+                if (CODES && st == 0 && (s0 & 4) == 0) issue_scales((s0 >> 3) + 1);
                 read_a(St{}, I1{}, I0{}); read_a(St{}, I1{}, I1{});
                 LRBI_SB();
-                mma(I0{}, I0{}, I0{}); read_b(St{}, I1{}, I0{});
+                mma(I0{}, I0{}, I0{}, St{}); read_b(St{}, I1{}, I0{});
                 LRBI_SB();
-                mma(I0{}, I0{}, I1{}); read_b(St{}, I1{}, I1{}); issue_piece(stp, I2{});
+                mma(I0{}, I0{}, I1{}, St{}); read_b(St{}, I1{}, I1{}); issue_piece(stp, I2{});
                 LRBI_SB();
-                mma(I0{}, I1{}, I0{}); read_b(St{}, I1{}, I2{}); issue_piece(stp, I3{});
+                mma(I0{}, I1{}, I0{}, St{}); read_b(St{}, I1{}, I2{}); issue_piece(stp, I3{});
                 LRBI_SB();
-                mma(I0{}, I1{}, I1{}); read_b(St{}, I1{}, I3{});
+                mma(I0{}, I1{}, I1{}, St{}); read_b(St{}, I1{}, I3{});
                 LRBI_SB();
-                mma(I0{}, I2{}, I0{}); mma(I0{}, I2{}, I1{}); mma(I0{}, I3{}, I0{}); mma(I0{}, I3{}, I1{});
-                wait_loads<(NS - 3) * 4>();
+                mma(I0{}, I2{}, I0{}, St{}); mma(I0{}, I2{}, I1{}, St{}); mma(I0{}, I3{}, I0{}, St{}); mma(I0{}, I3{}, I1{}, St{});
+                wait_loads<(NS - 3) * PIECES>();
                 LRBI_BARRIER();
                 read_a(St1{}, I0{}, I0{}); read_a(St1{}, I0{}, I1{});
                 LRBI_SB();
-                mma(I1{}, I0{}, I0{}); read_b(St1{}, I0{}, I0{});
+                mma(I1{}, I0{}, I0{}, St{}); read_b(St1{}, I0{}, I0{});
                 LRBI_SB();
-                mma(I1{}, I0{}, I1{}); read_b(St1{}, I0{}, I1{}); issue_piece(stn, I0{});
+                mma(I1{}, I0{}, I1{}, St{}); read_b(St1{}, I0{}, I1{}); issue_piece(stn, I0{});
                 LRBI_SB();
-                mma(I1{}, I1{}, I0{}); read_b(St1{}, I0{}, I2{}); issue_piece(stn, I1{});
+                mma(I1{}, I1{}, I0{}, St{}); read_b(St1{}, I0{}, I2{}); issue_piece(stn, I1{});
                 LRBI_SB();
-                mma(I1{}, I1{}, I1{}); read_b(St1{}, I0{}, I3{});
+                mma(I1{}, I1{}, I1{}, St{}); read_b(St1{}, I0{}, I3{});
                 LRBI_SB();
-                mma(I1{}, I2{}, I0{}); mma(I1{}, I2{}, I1{}); mma(I1{}, I3{}, I0{}); mma(I1{}, I3{}, I1{});
+                mma(I1{}, I2{}, I0{}, St{}); mma(I1{}, I2{}, I1{}, St{}); mma(I1{}, I3{}, I0{}, St{}); mma(I1{}, I3{}, I1{}, St{});
+                if constexpr (CODES) {
+                    if constexpr (st == NS - 2) read_scales(I1{}, s0 + NS);
+                    if constexpr (st == NS - 1)
+#pragma unroll
+                        for (int a = 0; a < 4; ++a) scales[0][a] = scales[1][a];
+                }
                 // the factor slices are older than slab 1, which every wavefront has waited for
                 if (st == 0 && s0 == 0) form_mask();
             }
@@ -323,19 +383,29 @@ bool grad256_wins(const Geom &g, int64_t N)
     return full && (N >= 768 || (N >= 512 && rounds * cus * 9 <= t256 * 10));
 }
 
-int launch_grad256(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, int64_t N,
-                   const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
+template <typename Tag, bool CODES>
+static int launch_grad256_t(const Geom &g, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales, int64_t ldxs,
+                            int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
 {
     const int64_t iblocks = (g.m + G256_B - 1) / G256_B, jblocks = (g.n + G256_B - 1) / G256_B;
     const int64_t blocks = iblocks * jblocks;
     if (blocks > 0x7FFFFFFF / G256_THREADS) return LRBI_ERR_SHAPE;
     const int w_vec_ok = (((uintptr_t)dDW & 15) == 0) && (lddw % 8 == 0);
-    auto kern = dt == LRBI_F16 ? mfma_grad256_kernel<F16Tag> : mfma_grad256_kernel<BF16Tag>;
-    LRBI_SET_MAX_LDS(kern, SmemG256::bytes);
-    LRBI_LAUNCH(kern, dim3((unsigned)blocks), dim3(G256_THREADS), SmemG256::bytes, stream, g, (const uint16_t *)dDY, lddy,
-                (const uint16_t *)dX, ldx, (int)N, dIp, dIz, (uint16_t *)dDW, lddw, (int)iblocks, (int)jblocks,
-                (blocks % 8 == 0) ? 1 : 0, w_vec_ok);
+    auto kern = mfma_grad256_kernel<Tag, CODES>;
+    constexpr size_t smem = SmemG256<CODES>::bytes;
+    LRBI_SET_MAX_LDS(kern, smem);
+    LRBI_LAUNCH(kern, dim3((unsigned)blocks), dim3(G256_THREADS), smem, stream, g, (const uint16_t *)dDY, lddy,
+                (const std::conditional_t<CODES, unsigned char, uint16_t> *)dX, ldx, (const unsigned char *)dXScales, ldxs, (int)N, dIp, dIz,
+                (uint16_t *)dDW, lddw, (int)iblocks, (int)jblocks, (blocks % 8 == 0) ? 1 : 0, w_vec_ok);
     return LRBI_OK;
+}
+int launch_grad256(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales,
+                   int64_t ldxs, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
+{
+#define LRBI_ARGS g, dDY, lddy, dX, ldx, dXScales, ldxs, N, dIp, dIz, dDW, lddw, stream
+    if (dt == LRBI_F16) return dXScales ? launch_grad256_t<F16Tag, true>(LRBI_ARGS) : launch_grad256_t<F16Tag, false>(LRBI_ARGS);
+    return dXScales ? launch_grad256_t<BF16Tag, true>(LRBI_ARGS) : launch_grad256_t<BF16Tag, false>(LRBI_ARGS);
+#undef LRBI_ARGS
 }
 
 } // namespace lrbi

@@ -160,3 +160,25 @@ def test_nan_codes_reach_their_weights():
         dW = lrbi.checkpoint_grad(d, torch.ones(32, 40, device=dev(), dtype=t), codes, scales, *device_factors(d, Ip01, Iz01))
         bad = torch.isnan(dW)
         assert bad[:, 5].sum() == 31 and bad.sum() == 31 and not bad[3, 5] and (dW[3] == 0).all()
+
+
+# large enough for 256 x 256 blocks; batches of few slabs of 32 columns, of eight and one more, of odd numbers of them
+@pytest.mark.parametrize("dtype,m,n,r,c,k,N", [("bf16", 4096, 4096, 512, 512, 32, 128), ("f16", 4096, 4096, 256, 256, 16, 288), ("bf16", 4096, 4096, 128, 64, 40, 544),
+                                               ("f16", 2304, 4096, 256, 256, 16, 1024), ("bf16", 4096, 9216, 256, 256, 16, 96)])
+def test_grad_of_large_layers(dtype, m, n, r, c, k, N):
+    print("checkpoint grad, large", dtype, m, n, r, c, k, N, flush=True)
+    rng = np.random.default_rng(N)
+    d = lrbi.Desc(m, n, r, c, k)
+    ip, iz = device_factors(d, *workloads.make_factors(rng, d.tiles, r, c, k, 0.15))
+    gen = torch.Generator(device=dev()).manual_seed(N)
+    X = (torch.randn(n, N, device=dev(), generator=gen) * torch.exp(torch.randn(n, 1, device=dev(), generator=gen))).to(TORCH_DTYPE[dtype])
+    dY = torch.randn(m, N, device=dev(), generator=gen).to(TORCH_DTYPE[dtype])
+    codes, scales = lrbi.checkpoint_pack(X)
+    Xq = lrbi.checkpoint_unpack(codes, scales, N, TORCH_DTYPE[dtype]).double()
+    got = lrbi.checkpoint_grad(d, dY, codes, scales, ip, iz).double()
+    bits = lrbi.decode_mask(d, ip, iz)
+    M = ((bits[:, :, None] >> torch.arange(8, device=dev(), dtype=torch.uint8)) & 1).reshape(m, -1)[:, :n].bool()
+    want, size = dY.double() @ Xq.T, dY.double().abs() @ Xq.abs().T
+    want[~M] = 0
+    assert (got[~M] == 0).all()
+    assert ((got - want).abs() <= HALF[dtype] * want.abs() + N * 2.0 ** -24 * size + 2.0 ** -25).all()
