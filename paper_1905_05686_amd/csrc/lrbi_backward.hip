@@ -23,7 +23,6 @@
 
 #include "lrbi_internal.hpp"
 #include "lrbi_mfma_common.hpp"
-#include "lrbi_store.hpp"
 
 namespace lrbi {
 
@@ -451,16 +450,9 @@ struct SmemG {
     static constexpr size_t bytes = (op_bytes > cs_bytes ? op_bytes : cs_bytes) + (size_t)ms_words * 4;
 };
 
-// Eight 8-bit codes as operands of the 16-bit products
-__device__ __forceinline__ uint4 widen_codes(F16Tag, uint2 w, float s) { return widen8_f16(w, s); }
-__device__ __forceinline__ uint4 widen_codes(BF16Tag, uint2 w, float s) { return widen8_bf16(w, s); }
-
-// CODES: X is an activation checkpoint (8-bit codes, XS its scale bytes): eight bytes instead of sixteen per lane and piece,
-// widened, exactly, on their way into LDS.  VEC then speaks of dY alone (the codes are always whole aligned blocks).
-template <typename Tag, bool VEC, bool CODES>
+template <typename Tag, bool VEC>
 __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const uint16_t *__restrict__ DY, int64_t lddy,
-                                                                const std::conditional_t<CODES, unsigned char, uint16_t> *__restrict__ X,
-                                                                int64_t ldx, const unsigned char *__restrict__ XS, int64_t ldxs, int N,
+                                                                const uint16_t *__restrict__ X, int64_t ldx, int N,
                                                                 const uint32_t *__restrict__ Ip,
                                                                 const uint32_t *__restrict__ Iz,
                                                                 uint16_t *__restrict__ DW, int64_t lddw, int jblocks,
@@ -499,12 +491,6 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
         if (row < rows) {
             if (VEC) {
                 if (qq < N) v = *reinterpret_cast<const uint4 *>(base + row * ld + qq); // N % 8 == 0
-            } else if (CODES && qq + 8 <= N) { // 16 bytes at any element's address
-                struct __attribute__((packed, aligned(2))) Unaligned {
-                    uint32_t x, y, z, w;
-                };
-                const Unaligned u = *reinterpret_cast<const Unaligned *>(base + row * ld + qq);
-                v = make_uint4(u.x, u.y, u.z, u.w);
             } else {
                 uint16_t tmp[8];
 #pragma unroll
@@ -525,18 +511,6 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
     const uint32_t lda2 = (uint32_t)(lddy * 2), ldb2 = (uint32_t)(ldx * 2);
     const char *abase0 = (const char *)(DY + i0 * lddy);
     const char *bbase0 = (const char *)(X + (int64_t)j0 * ldx);
-    // the checkpoint's piece of a row: its codes and its scale (columns past N: zeros, at any scale)
-    auto load_codes = [&](int row, int k0) -> uint4 {
-        const int q = k0 + (tid & 7) * 8;
-        if constexpr (CODES) {
-            const int64_t j = (int64_t)j0 + (row < b_last ? row : b_last);
-            if (q < N) {
-                const uint2 w = *reinterpret_cast<const uint2 *>(X + j * ldx + q);
-                return make_uint4(w.x, w.y, (uint32_t)XS[j * ldxs + (q >> 5)], 0u);
-            }
-        }
-        return make_uint4(0u, 0u, 0u, 0u);
-    };
     int cols_left = 0; // batch columns from the first one of the slab whose pieces sit in areg / breg
     auto load_slab = [&](int slab) {
         const int k0 = slab * BK;
@@ -549,8 +523,7 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
                 const int row = row0 + 32 * c;
                 const uint32_t ar = (uint32_t)(row < a_last ? row : a_last), br = (uint32_t)(row < b_last ? row : b_last);
                 areg[c] = *reinterpret_cast<const uint4 *>(abase + (ar * lda2 + off));
-                if constexpr (CODES) breg[c] = load_codes(row, k0);
-                else breg[c] = *reinterpret_cast<const uint4 *>(bbase + (br * ldb2 + off));
+                breg[c] = *reinterpret_cast<const uint4 *>(bbase + (br * ldb2 + off));
             }
         } else {
 #pragma unroll
@@ -558,8 +531,7 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
                 const int id = tid + kBwdThreads * c;
                 const int row = id >> 3, kc = id & 7;
                 areg[c] = load_piece(DY, lddy, i0 + row, g.m, k0 + kc * 8);
-                if constexpr (CODES) breg[c] = load_codes(row, k0);
-                else breg[c] = load_piece(X, ldx, (int64_t)j0 + row, g.n, k0 + kc * 8);
+                breg[c] = load_piece(X, ldx, (int64_t)j0 + row, g.n, k0 + kc * 8);
             }
         }
         cols_left = N - k0;
@@ -575,9 +547,8 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
             if (VEC) {
                 const bool col_ok = kc * 8 < cols_left;
                 if (!(row <= a_last && col_ok)) av = make_uint4(0u, 0u, 0u, 0u);
-                if (!CODES && !(row <= b_last && col_ok)) bv = make_uint4(0u, 0u, 0u, 0u);
+                if (!(row <= b_last && col_ok)) bv = make_uint4(0u, 0u, 0u, 0u);
             }
-            if constexpr (CODES) bv = widen_codes(Tag{}, make_uint2(bv.x, bv.y), scale_operand(bv.z));
             *reinterpret_cast<uint4 *>(as + row * OP_STRIDE + kc * 8) = av;
             *reinterpret_cast<uint4 *>(bs + row * OP_STRIDE + kc * 8) = bv;
         }
@@ -604,8 +575,7 @@ __global__ __launch_bounds__(kBwdThreads) void mfma_grad_kernel(Geom g, const ui
     // 64 columns may lie in the next tile column; words 2 and 3 of the I_z rows and a second set of I_p words (behind
     // the first one: one word per row) then come from that tile.
     const bool half = (g.c % BJ) != 0 && (g.c % 64) == 0 && g.k <= 32;
-    // (a tile that the matrix cuts off has whole factors all the same, and what lies outside is not stored)
-    const bool lined_up = ((g.c % BJ) == 0 || half) && (g.r % BI) == 0 && g.k <= FAST_MAX_K && (CODES || !g.ragged);
+    const bool lined_up = ((g.c % BJ) == 0 || half) && (g.r % BI) == 0 && g.k <= FAST_MAX_K && !g.ragged;
     if (lined_up) {
         const int ti = (int)(i0 / g.r), tj = j0 / g.c;
         const int il0 = (int)(i0 - (int64_t)ti * g.r), coff = j0 - tj * g.c;
@@ -832,40 +802,35 @@ int launch_gemm_t(const Geom &g, const BwdPlan &plan, lrbi_dtype dt, const void 
 #undef LRBI_T_ARGS
 }
 
-int launch_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales,
-                int64_t ldxs, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
+int launch_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx,
+                int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
 {
-    if (dt == LRBI_F32) return launch_f32_grad(g, (const float *)dDY, lddy, dX, ldx, dXScales, ldxs, N, dIp, dIz, (float *)dDW, lddw, stream);
+    if (dt == LRBI_F32)
+        return launch_f32_grad(g, (const float *)dDY, lddy, (const float *)dX, ldx, N, dIp, dIz, (float *)dDW, lddw, stream);
     if (grad256_wins(g, N) && grad256_ok(g, dDY, lddy, dX, ldx, N))
-        return launch_grad256(g, dt, dDY, lddy, dX, ldx, dXScales, ldxs, N, dIp, dIz, dDW, lddw, stream);
+        return launch_grad256(g, dt, dDY, lddy, dX, ldx, nullptr, 0, N, dIp, dIz, dDW, lddw, stream);
     const int64_t iblocks = (g.m + 127) / 128, jblocks = (g.n + BJ - 1) / BJ;
     const int64_t blocks = iblocks * jblocks;
     if (blocks > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    bool vec = (((uintptr_t)dDY & 15) == 0) && (lddy % 8 == 0) && (N % 8 == 0) && lddy < ((int64_t)1 << 22);
-    if (!dXScales) vec = vec && (((uintptr_t)dX & 15) == 0) && (ldx % 8 == 0) && ldx < ((int64_t)1 << 22);
+    const bool vec = (((uintptr_t)dDY & 15) == 0) && (lddy % 8 == 0) && (((uintptr_t)dX & 15) == 0) && (ldx % 8 == 0) &&
+                     (N % 8 == 0) && lddy < ((int64_t)1 << 22) && ldx < ((int64_t)1 << 22);
     const int w_vec_ok = (((uintptr_t)dDW & 15) == 0) && (lddw % 8 == 0);
     const size_t smem = SmemG::bytes;
-#define LRBI_LAUNCH_G(TAG, V, CODES, X)                                                                            \
+#define LRBI_LAUNCH_G(TAG, V)                                                                                      \
     do {                                                                                                           \
-        auto kern = mfma_grad_kernel<TAG, V, CODES>;                                                               \
+        auto kern = mfma_grad_kernel<TAG, V>;                                                                      \
         LRBI_SET_MAX_LDS(kern, smem);                                                                              \
-        LRBI_LAUNCH(kern, dim3((unsigned)blocks), dim3(kBwdThreads), smem, stream, g, (const uint16_t *)dDY,       \
-                    lddy, X, ldx, (const unsigned char *)dXScales, ldxs, (int)N, dIp, dIz, (uint16_t *)dDW, lddw,  \
-                    (int)jblocks, w_vec_ok);                                                                       \
-    } while (0)
-#define LRBI_LAUNCH_GX(TAG, V)                                                                                     \
-    do {                                                                                                           \
-        if (dXScales) LRBI_LAUNCH_G(TAG, V, true, (const unsigned char *)dX);                                      \
-        else LRBI_LAUNCH_G(TAG, V, false, (const uint16_t *)dX);                                                   \
+        LRBI_LAUNCH(kern, dim3((unsigned)blocks), dim3(kBwdThreads), smem, stream, g, (const uint16_t *)dDY, \
+                           lddy, (const uint16_t *)dX, ldx, (int)N, dIp, dIz, (uint16_t *)dDW, lddw, (int)jblocks,  \
+                           w_vec_ok);                                                                              \
     } while (0)
     if (dt == LRBI_F16) {
-        if (vec) LRBI_LAUNCH_GX(F16Tag, true);
-        else LRBI_LAUNCH_GX(F16Tag, false);
+        if (vec) LRBI_LAUNCH_G(F16Tag, true);
+        else LRBI_LAUNCH_G(F16Tag, false);
     } else {
-        if (vec) LRBI_LAUNCH_GX(BF16Tag, true);
-        else LRBI_LAUNCH_GX(BF16Tag, false);
+        if (vec) LRBI_LAUNCH_G(BF16Tag, true);
+        else LRBI_LAUNCH_G(BF16Tag, false);
     }
-#undef LRBI_LAUNCH_GX
 #undef LRBI_LAUNCH_G
     return LRBI_OK;
 }

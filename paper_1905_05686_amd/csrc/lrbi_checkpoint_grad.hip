@@ -1,0 +1,358 @@
+// Weight gradient dW = (dY Xq^T) o I_a from an activation checkpoint, on the matrix cores: any shape, alignment and type (long
+// batches of lined-up shapes go to the 256 x 256 form, lrbi_grad256.hip).
+//
+// A short batch makes the output most of the work (4096 x 9216, batch 128: 75 MB of dW, 2 MB read), so the kernel is built to keep
+// stores flowing: a workgroup takes 128 x 128 blocks of dW one after the other, and while a block is multiplied, masked and
+// written the first operands of the next one are on their way; its four wavefronts own 64 x 64 each, mask and write them on their own,
+// and wait for each other only when a slab of 64 batch columns changes hands.
+//   * dY: 16 bytes a load at any element's address, staged in LDS as [row][batch].
+//   * X: staged as codes, widened by the conversion instruction that also applies the scale, exactly, when they are read.
+//   * fp32 dY is split into three bf16 parts, y = y1 + y2 + y3 exactly; a checkpoint's values are bf16 numbers, so three 16-bit
+//     products, exact in fp32, do the work of sixteen times slower fp32 ones.
+//   * mask: tile sizes that are multiples of 64 and ranks up to 64: each wavefront fetches its block's slices of the factors before
+//     the products and forms its words behind them (Eq. 3); other shapes word by word.
+#include <type_traits>
+
+#include "lrbi_internal.hpp"
+#include "lrbi_mfma_common.hpp"
+#include "lrbi_store.hpp"
+
+namespace lrbi {
+
+static constexpr int CG_THREADS = 256;
+static constexpr int CG_B = 128;            // rows and columns of a block of dW
+static constexpr int CG_K = 64;             // batch columns per slab: two blocks of codes
+static constexpr int CG_A_ROW = CG_K + 8;   // halfs of a staged row of dY
+static constexpr int CG_X_ROW = CG_K + 16;  // bytes of a staged row of X
+static constexpr int CG_C_ROW = 64 + 4;     // halfs of a row of a wavefront's strip of output
+
+struct F32Tag {};
+template <typename Tag> struct CgTypes {
+    typedef uint16_t elem;
+    typedef Tag op;
+    static constexpr int parts = 1, waves = 3; // wavefronts a SIMD: workgroups that share a compute unit
+};
+template <> struct CgTypes<F32Tag> {
+    typedef float elem;
+    typedef BF16Tag op;
+    static constexpr int parts = 3, waves = 2;
+};
+template <typename Tag> struct SmemCg {
+    static constexpr int a_bytes = CG_B * CG_A_ROW * 2; // of one part
+    static constexpr int x_off = CgTypes<Tag>::parts * a_bytes;
+    static constexpr int s_off = x_off + CG_B * CG_X_ROW;  // [128 rows][2 blocks] scales as conversion operands
+    static constexpr int w_off = s_off + CG_B * 2 * 4;     // per wavefront: factor slice [64][2], mask words [64][2]
+    static constexpr int c_off = w_off + 4 * 2 * 64 * 8;   // per wavefront: 32 rows of output (16-bit types)
+    static constexpr int bytes = c_off + (CgTypes<Tag>::parts == 1 ? 4 * 32 * CG_C_ROW * 2 : 0);
+};
+
+__device__ __forceinline__ uint4 cg_widen(F16Tag, uint2 w, float s) { return widen8_f16(w, s); }
+__device__ __forceinline__ uint4 cg_widen(BF16Tag, uint2 w, float s) { return widen8_bf16(w, s); }
+
+// to nearest even, as the conversion instruction has it
+__device__ __forceinline__ uint16_t cg_narrow(F16Tag, float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+__device__ __forceinline__ uint16_t cg_narrow(BF16Tag, float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+
+// 16 bytes of a row at any element's address, columns q on: zeros from column N on.  A piece that the row's end cuts off is read as
+// the row's last 16 bytes and moved down.
+template <typename E> __device__ __forceinline__ uint4 cg_load(const E *row, int q, int N, bool whole)
+{
+    constexpr int U = 16 / sizeof(E);
+    struct __attribute__((packed, aligned(sizeof(E)))) Piece {
+        uint64_t lo, hi;
+    };
+    uint64_t lo = 0, hi = 0;
+    if (N >= U) {
+        const int from = q < N - U ? q : N - U;
+        const Piece p = *reinterpret_cast<const Piece *>(row + from);
+        lo = p.lo;
+        hi = p.hi;
+        if (!whole) {
+            const int s = (q - from) * (int)sizeof(E) * 8; // bits
+            lo = s >= 64 ? hi >> (s & 63) : s ? lo >> s | hi << (64 - s) : lo;
+            hi = s >= 64 ? 0 : hi >> s;
+            if (s >= 128) lo = 0;
+        }
+    } else {
+#pragma unroll 1
+        for (int e = 0; e < U && q + e < N; ++e) {
+            uint64_t v = 0;
+            __builtin_memcpy(&v, row + q + e, sizeof(E));
+            const int s = e * (int)sizeof(E) * 8;
+            if (s < 64) lo |= v << s;
+            else hi |= v << (s - 64);
+        }
+    }
+    return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
+template <typename Tag>
+__global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_grad_kernel(Geom g, const typename CgTypes<Tag>::elem *__restrict__ DY, int64_t lddy,
+                                                                     const unsigned char *__restrict__ X, int64_t ldx,
+                                                                     const unsigned char *__restrict__ XS, int64_t ldxs, int N,
+                                                                     const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz,
+                                                                     typename CgTypes<Tag>::elem *__restrict__ DW, int64_t lddw,
+                                                                     int64_t jblocks, int64_t blocks, int w_vec_ok)
+{
+    typedef typename CgTypes<Tag>::elem E;
+    typedef typename CgTypes<Tag>::op Op;
+    constexpr int PARTS = CgTypes<Tag>::parts;
+    using S = SmemCg<Tag>;
+    extern __shared__ uint4 lrbi_dyn_smem[];
+    unsigned char *smem = (unsigned char *)lrbi_dyn_smem;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave >> 1, wj = wave & 1;
+    const int l32 = lane & 31, lg = lane >> 5;
+    uint32_t *fz = (uint32_t *)(smem + S::w_off + wave * 1024), *mask = fz + 128;
+    const int nslabs = (N + CG_K - 1) / CG_K;
+    const bool lined_up = g.c % 64 == 0 && g.r % 64 == 0 && g.k <= FAST_MAX_K;
+
+    // a slab on its way: lane = (row tid / 8 + 32 c, eight columns tid % 8) of dY, (row tid / 4 + 64 c, 16 columns tid % 4) of X
+    constexpr int AV = sizeof(E) / 2; // 16-byte pieces of eight elements
+    uint4 areg[4][AV];
+    uint4 xreg[2];
+    uint32_t sreg; // two bytes
+    auto load = [&](int64_t block, int slab) __attribute__((always_inline)) {
+        const int64_t ib = block / jblocks, i0 = ib * CG_B, j0 = (block - ib * jblocks) * CG_B;
+        const int q = slab * CG_K + (tid & 7) * 8;
+        const bool whole = (slab + 1) * CG_K <= N;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int64_t i = i0 + (tid >> 3) + 32 * c, row = i < g.m ? i : g.m - 1; // (rows past the matrix are not stored)
+#pragma unroll
+            for (int k = 0; k < AV; ++k) areg[c][k] = cg_load(DY + row * lddy, q + k * (16 / (int)sizeof(E)), N, whole);
+        }
+        const int p = slab * CG_K + (tid & 3) * 16;
+        sreg = 0;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int64_t j = j0 + (tid >> 2) + 64 * c, row = j < g.n ? j : g.n - 1;
+            xreg[c] = make_uint4(0u, 0u, 0u, 0u);
+            if (p < N) { // a block is whole, zeros behind column N
+                xreg[c] = *reinterpret_cast<const uint4 *>(X + row * ldx + p);
+                sreg |= (uint32_t)XS[row * ldxs + (p >> 5)] << (8 * c);
+            }
+        }
+    };
+    auto stage = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            unsigned char *dst = smem + ((tid >> 3) + 32 * c) * (CG_A_ROW * 2) + (tid & 7) * 16;
+            if constexpr (PARTS == 1) {
+                *reinterpret_cast<uint4 *>(dst) = areg[c][0];
+            } else {
+                uint32_t parts[3][4], y8[8];
+                __builtin_memcpy(y8, areg[c], 32);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    // cut off, not rounded: 8 of the 24 bits each; an infinity or a NaN is its first part alone
+                    uint32_t h[3][2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t u = y8[2 * k + e];
+                        float y = __builtin_bit_cast(float, u);
+                        const bool finite = __builtin_fabsf(y) < __builtin_inff();
+                        if (!finite) u |= (u & 0x7FFFFFu) ? 0x400000u : 0u;
+                        h[0][e] = u >> 16;
+                        y -= __builtin_bit_cast(float, u & 0xFFFF0000u);
+                        u = finite ? __builtin_bit_cast(uint32_t, y) : 0u;
+                        h[1][e] = u >> 16;
+                        y -= __builtin_bit_cast(float, u & 0xFFFF0000u);
+                        h[2][e] = finite ? __builtin_bit_cast(uint32_t, y) >> 16 : 0u;
+                    }
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) parts[q][k] = h[q][0] | h[q][1] << 16;
+                }
+#pragma unroll
+                for (int q = 0; q < 3; ++q)
+                    *reinterpret_cast<uint4 *>(dst + q * S::a_bytes) = make_uint4(parts[q][0], parts[q][1], parts[q][2], parts[q][3]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int row = (tid >> 2) + 64 * c;
+            *reinterpret_cast<uint4 *>(smem + S::x_off + row * CG_X_ROW + (tid & 3) * 16) = xreg[c];
+            if ((tid & 1) == 0) *reinterpret_cast<uint32_t *>(smem + S::s_off + row * 8 + ((tid >> 1) & 1) * 4) = (sreg >> (8 * c) & 255u) << 23;
+        }
+    };
+
+    int64_t block = blockIdx.x;
+    load(block, 0);
+#pragma unroll 1
+    for (; block < blocks; block += gridDim.x) {
+        const int64_t next = block + gridDim.x;
+        const int64_t ib = block / jblocks;
+        // this wavefront's 64 x 64
+        const int64_t i0 = ib * CG_B + wi * 64, j0 = (block - ib * jblocks) * CG_B + wj * 64;
+        // ---- factors under it, or its mask words: lane = row
+        uint32_t z[2] = {0u, 0u}, p[2] = {0u, 0u}, words[2] = {0u, 0u};
+        if (i0 < g.m && j0 < g.n) {
+            if (lined_up) { // (a tile that the matrix cuts off has whole factors; what lies outside is not stored)
+                const int ti = (int)(i0 / g.r), tj = (int)(j0 / g.c);
+                const int64_t t = (int64_t)ti * g.tile_cols + tj;
+                const int il = (int)(i0 - (int64_t)ti * g.r) + lane, zw = (int)((j0 - (int64_t)tj * g.c) >> 5);
+                if (lane < g.k) {
+                    const u32x2 v = *reinterpret_cast<const u32x2 *>(Iz + (t * g.k + lane) * g.izw + zw);
+                    z[0] = v.x;
+                    z[1] = v.y;
+                }
+                p[0] = Ip[(t * g.r + il) * g.ipw];
+                if (g.ipw > 1) p[1] = Ip[(t * g.r + il) * g.ipw + 1];
+            } else if (i0 + lane < g.m) {
+                const int ti = (int)((i0 + lane) / g.r), il = (int)(i0 + lane - (int64_t)ti * g.r);
+#pragma unroll
+                for (int w = 0; w < 2; ++w) words[w] = decode_word<true>(g, Ip, Iz, ti, il, (int)(j0 >> 5) + w);
+            }
+        }
+        // ---- products
+        f32x16 acc[2][2];
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
+#pragma unroll 1
+        for (int s = 0; s < nslabs; ++s) {
+            __syncthreads(); // the slab before has been read
+            stage();
+            const bool more = s + 1 < nslabs;
+            if (more || next < blocks) load(more ? block : next, more ? s + 1 : 0);
+            __syncthreads();
+            const unsigned char *as = smem + (wi * 64 + l32) * (CG_A_ROW * 2) + 16 * lg;
+            const unsigned char *xs = smem + S::x_off + (wj * 64 + l32) * CG_X_ROW + 8 * lg;
+            const unsigned char *ss = smem + S::s_off + (wj * 64 + l32) * 8;
+            float sc[2];
+#pragma unroll
+            for (int kk = 0; kk < CG_K / 16; ++kk) {
+                uint4 xf[2], yf[2];
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    if (kk % 2 == 0) sc[a] = *reinterpret_cast<const float *>(ss + a * 32 * 8 + kk * 2);
+                    xf[a] = cg_widen(Op{}, *reinterpret_cast<const uint2 *>(xs + a * 32 * CG_X_ROW + kk * 16), sc[a]);
+                }
+#pragma unroll
+                for (int part = PARTS - 1; part >= 0; --part) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        yf[b] = *reinterpret_cast<const uint4 *>(as + part * S::a_bytes + b * 32 * (CG_A_ROW * 2) + kk * 32);
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) acc[a][b] = mfma_32x32x16(Op{}, xf[a], yf[b], acc[a][b]);
+                }
+            }
+        }
+        // ---- mask words of row `lane`
+        if (lined_up) {
+            wave_fence();
+            *reinterpret_cast<u32x2 *>(fz + lane * 2) = u32x2{z[0], z[1]};
+            wave_fence();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                for (uint32_t sel = p[h]; sel; sel &= sel - 1u) {
+                    const u32x2 v = *reinterpret_cast<const u32x2 *>(fz + (__builtin_ctz(sel) + 32 * h) * 2);
+                    words[0] |= v.x;
+                    words[1] |= v.y;
+                }
+        }
+        // ---- masked output: per 32 x 32 block the lane holds row l32 (of dW) and columns 8 * (v / 4) + 4 * lg + (v % 4)
+        if constexpr (PARTS == 1) {
+            wave_fence();
+            *reinterpret_cast<u32x2 *>(mask + lane * 2) = u32x2{words[0], words[1]};
+            uint16_t *strip = (uint16_t *)(smem + S::c_off) + wave * (32 * CG_C_ROW);
+            const unsigned char *mb = (const unsigned char *)mask;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                wave_fence();
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int v4 = 0; v4 < 4; ++v4) {
+                        uint16_t o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = cg_narrow(Op{}, acc[a][b][4 * v4 + e]);
+                        uint2 w;
+                        __builtin_memcpy(&w, o, 8);
+                        *reinterpret_cast<uint2 *>(strip + l32 * CG_C_ROW + a * 32 + 8 * v4 + 4 * lg) = w;
+                    }
+                wave_fence();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { // eight rows an instruction, 128 bytes each
+                    const int rr = 8 * q + (lane >> 3), pc = lane & 7;
+                    const uint2 lo = *reinterpret_cast<const uint2 *>(strip + rr * CG_C_ROW + pc * 8);
+                    const uint2 hi = *reinterpret_cast<const uint2 *>(strip + rr * CG_C_ROW + pc * 8 + 4);
+                    const uint4 v = apply_mask8(make_uint4(lo.x, lo.y, hi.x, hi.y), (uint32_t)mb[(b * 32 + rr) * 8 + pc]);
+                    const int64_t i = i0 + b * 32 + rr, j = j0 + pc * 8;
+                    if (i >= g.m || j >= g.n) continue;
+                    E *dst = DW + i * lddw + j;
+                    if (w_vec_ok && j + 8 <= g.n) {
+                        *reinterpret_cast<uint4 *>(dst) = v;
+                    } else {
+                        const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (j + e < g.n) dst[e] = (uint16_t)(w4[e >> 1] >> (16 * (e & 1)));
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int64_t i = i0 + b * 32 + l32;
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    const uint32_t word = __shfl(words[a], b * 32 + l32, 64);
+#pragma unroll
+                    for (int v4 = 0; v4 < 4; ++v4) {
+                        float o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = ((word >> (8 * v4 + 4 * lg + e)) & 1u) ? acc[a][b][4 * v4 + e] : 0.f;
+                        const int64_t j = j0 + a * 32 + 8 * v4 + 4 * lg;
+                        if (i >= g.m || j >= g.n) continue;
+                        E *dst = DW + i * lddw + j;
+                        if (w_vec_ok && j + 4 <= g.n) {
+                            *reinterpret_cast<float4 *>(dst) = make_float4(o[0], o[1], o[2], o[3]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (j + e < g.n) dst[e] = o[e];
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <typename Tag>
+static int launch_t(const Geom &g, const void *dDY, int64_t lddy, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t N,
+                    const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
+{
+    typedef typename CgTypes<Tag>::elem E;
+    const int64_t iblocks = (g.m + CG_B - 1) / CG_B, jblocks = (g.n + CG_B - 1) / CG_B, blocks = iblocks * jblocks;
+    const int64_t at_once = CgTypes<Tag>::waves * (int64_t)compute_units_of(stream);
+    const int64_t groups = blocks < at_once ? blocks : at_once;
+    const int w_vec_ok = ((uintptr_t)dDW & 15) == 0 && lddw * (int64_t)sizeof(E) % 16 == 0;
+    auto kern = checkpoint_grad_kernel<Tag>;
+    LRBI_SET_MAX_LDS(kern, SmemCg<Tag>::bytes);
+    LRBI_LAUNCH(kern, dim3((unsigned)groups), dim3(CG_THREADS), SmemCg<Tag>::bytes, stream, g, (const E *)dDY, lddy, (const unsigned char *)dCodes,
+                ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, jblocks, blocks, w_vec_ok);
+    return LRBI_OK;
+}
+
+int launch_checkpoint_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dCodes, int64_t ldc, const void *dScales,
+                           int64_t lds, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
+{
+    if (dt != LRBI_F32 && grad256_wins(g, N) && grad256_ok(g, dDY, lddy, dCodes, ldc, N))
+        return launch_grad256(g, dt, dDY, lddy, dCodes, ldc, dScales, lds, N, dIp, dIz, dDW, lddw, stream);
+#define LRBI_ARGS g, dDY, lddy, dCodes, ldc, dScales, lds, N, dIp, dIz, dDW, lddw, stream
+    switch (dt) {
+    case LRBI_F32: return launch_t<F32Tag>(LRBI_ARGS);
+    case LRBI_F16: return launch_t<F16Tag>(LRBI_ARGS);
+    default: return launch_t<BF16Tag>(LRBI_ARGS);
+    }
+#undef LRBI_ARGS
+}
+
+} // namespace lrbi

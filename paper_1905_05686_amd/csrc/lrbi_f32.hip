@@ -21,10 +21,7 @@
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
-#include <type_traits>
-
 #include "lrbi_internal.hpp"
-#include "lrbi_store.hpp"
 
 namespace lrbi {
 
@@ -335,11 +332,9 @@ __global__ __launch_bounds__(64 * WAVES) void f32_gemm_kernel(Geom g, const floa
 // dW = (dY X^T) o I_a, fp32.  One wavefront per 32 x (32 NJ) block of dW (no reduction is split: the blocks are many
 // and the batch is short).  Both operands are read four batch columns at a time, in the order described above.
 // AHEAD: the mask words formed with four I_z rows in flight.
-// CODES: X is an activation checkpoint (8-bit codes, XS its scale bytes), read four codes at a time; VEC speaks of dY alone.
-template <int NJ, bool VEC, bool AHEAD, bool CODES>
+template <int NJ, bool VEC, bool AHEAD>
 __global__ __launch_bounds__(256) void f32_grad_kernel(Geom g, const float *__restrict__ DY, int64_t lddy,
-                                                       const std::conditional_t<CODES, unsigned char, float> *__restrict__ X, int64_t ldx,
-                                                       const unsigned char *__restrict__ XS, int64_t ldxs, int64_t N,
+                                                       const float *__restrict__ X, int64_t ldx, int64_t N,
                                                        const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz,
                                                        float *__restrict__ DW, int64_t lddw, int64_t jblocks, int64_t blocks)
 {
@@ -348,21 +343,9 @@ __global__ __launch_bounds__(256) void f32_grad_kernel(Geom g, const float *__re
     if (blk >= blocks) return; // whole wavefront; no barrier below
     const int64_t ib = blk / jblocks, i0 = 32 * ib, j0 = 32 * NJ * (blk - ib * jblocks);
     const float *yrow = DY + at_most(i0 + li, g.m - 1) * lddy;
-    const std::conditional_t<CODES, unsigned char, float> *xrow[NJ];
-    const unsigned char *srow[NJ];
+    const float *xrow[NJ];
 #pragma unroll
-    for (int b = 0; b < NJ; ++b) {
-        const int64_t j = at_most(j0 + 32 * b + li, g.n - 1);
-        xrow[b] = X + j * ldx;
-        srow[b] = XS + j * ldxs;
-    }
-    const auto load_codes = [&](int b, int64_t q, float (&v)[4]) { // q: a multiple of 4; the last block is whole, zeros behind column N
-        const bool in = q < N;
-        const uint32_t w = in ? *reinterpret_cast<const uint32_t *>(xrow[b] + q) : 0u;
-        const float s = scale_operand(in ? (uint32_t)srow[b][q >> 5] : 127u);
-        const store_f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
-        v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
-    };
+    for (int b = 0; b < NJ; ++b) xrow[b] = X + at_most(j0 + 32 * b + li, g.n - 1) * ldx;
     const auto load4 = [&](const float *p, int64_t q, float (&v)[4]) {
         if (VEC) {
             if (q < N) {
@@ -383,10 +366,7 @@ __global__ __launch_bounds__(256) void f32_grad_kernel(Geom g, const float *__re
     const auto load = [&](int64_t q, float (&yv)[4], float (&xv)[NJ][4]) { // past the last batch column: zeros, nothing is read
         load4(yrow, q + 4 * half, yv);
 #pragma unroll
-        for (int b = 0; b < NJ; ++b) {
-            if constexpr (CODES) load_codes(b, q + 4 * half, xv[b]);
-            else load4(xrow[b], q + 4 * half, xv[b]);
-        }
+        for (int b = 0; b < NJ; ++b) load4(xrow[b], q + 4 * half, xv[b]);
     };
     const auto mma = [&](float (&yv)[4], float (&xv)[NJ][4], f32x16_t (&c)[NJ]) {
 #pragma unroll
@@ -485,8 +465,8 @@ int launch_f32_gemm(const Geom &g, const float *dW, int64_t ldw, const uint32_t 
     return LRBI_OK;
 }
 
-int launch_f32_grad(const Geom &g, const float *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales, int64_t ldxs,
-                    int64_t N, const uint32_t *dIp, const uint32_t *dIz, float *dDW, int64_t lddw, hipStream_t stream)
+int launch_f32_grad(const Geom &g, const float *dDY, int64_t lddy, const float *dX, int64_t ldx, int64_t N,
+                    const uint32_t *dIp, const uint32_t *dIz, float *dDW, int64_t lddw, hipStream_t stream)
 {
     const int64_t iblocks = (g.m + 31) / 32;
     // two column blocks per wavefront share its reads of dY; one, while that leaves fewer than two wavefronts per SIMD
@@ -494,30 +474,22 @@ int launch_f32_grad(const Geom &g, const float *dDY, int64_t lddy, const void *d
     const int64_t jblocks = (g.n + 32 * nj - 1) / (32 * nj), blocks = iblocks * jblocks;
     if ((blocks + 3) / 4 > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
     const dim3 grid((unsigned)((blocks + 3) / 4));
-    bool vec = ((uintptr_t)dDY & 15) == 0 && lddy % 4 == 0 && N % 4 == 0;
-    if (!dXScales) vec = vec && ((uintptr_t)dX & 15) == 0 && ldx % 4 == 0;
+    const bool vec = (((uintptr_t)dDY | (uintptr_t)dX) & 15) == 0 && lddy % 4 == 0 && ldx % 4 == 0 && N % 4 == 0;
     // I_z rows ahead unless a word has several tiles, with few rows set in each (us, without and with: 2000 x 2000 in 5 x 5 tiles, rank
     // 2, 8 columns 13.0 / 16.5, 1000 x 4000 in 100 x 31, rank 40 11.4 / 12.5; a kernel of its own: a test in it took 5 % of the other shapes)
     const bool ahead = g.c >= 32;
-#define LRBI_LAUNCH_F32(NJ, V, CODES, X)                                                                           \
+#define LRBI_LAUNCH_F32(NJ, V)                                                                                     \
     do {                                                                                                           \
-        auto kern = ahead ? f32_grad_kernel<NJ, V, true, CODES> : f32_grad_kernel<NJ, V, false, CODES>;            \
-        LRBI_LAUNCH(kern, grid, dim3(256), 0, stream, g, dDY, lddy, X, ldx, (const unsigned char *)dXScales, ldxs, N, dIp, dIz, dDW, lddw, \
-                    jblocks, blocks);                                                                              \
-    } while (0)
-#define LRBI_LAUNCH_F32X(NJ, V)                                                                                    \
-    do {                                                                                                           \
-        if (dXScales) LRBI_LAUNCH_F32(NJ, V, true, (const unsigned char *)dX);                                     \
-        else LRBI_LAUNCH_F32(NJ, V, false, (const float *)dX);                                                     \
+        auto kern = ahead ? f32_grad_kernel<NJ, V, true> : f32_grad_kernel<NJ, V, false>;                          \
+        LRBI_LAUNCH(kern, grid, dim3(256), 0, stream, g, dDY, lddy, dX, ldx, N, dIp, dIz, dDW, lddw, jblocks, blocks); \
     } while (0)
     if (nj == 2) {
-        if (vec) LRBI_LAUNCH_F32X(2, true);
-        else LRBI_LAUNCH_F32X(2, false);
+        if (vec) LRBI_LAUNCH_F32(2, true);
+        else LRBI_LAUNCH_F32(2, false);
     } else {
-        if (vec) LRBI_LAUNCH_F32X(1, true);
-        else LRBI_LAUNCH_F32X(1, false);
+        if (vec) LRBI_LAUNCH_F32(1, true);
+        else LRBI_LAUNCH_F32(1, false);
     }
-#undef LRBI_LAUNCH_F32X
 #undef LRBI_LAUNCH_F32
     return LRBI_OK;
 }

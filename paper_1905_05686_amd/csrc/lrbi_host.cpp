@@ -631,7 +631,7 @@ extern "C" int lrbi_masked_grad(const lrbi_desc *desc, lrbi_dtype dtype, const v
     const Geom g = make_geom(desc);
     // matrix cores for every type at any batch (below 8 columns the slab is mostly zero fill); dW rows need not be 16-byte
     // aligned (the kernel then writes element by element)
-    return launch_grad(g, dtype, dDY, lddy, dX, ldx, nullptr, 0, N, (const uint32_t *)dIp_packed,
+    return launch_grad(g, dtype, dDY, lddy, dX, ldx, N, (const uint32_t *)dIp_packed,
                        (const uint32_t *)dIz_packed, dDW, lddw, (hipStream_t)stream);
 }
 
@@ -836,8 +836,8 @@ extern "C" int lrbi_checkpoint_grad(const lrbi_desc *desc, lrbi_dtype dtype, con
     if (!aligned_to(dDW, (uintptr_t)es) || !aligned_to(dDY, (uintptr_t)es)) return LRBI_ERR_ALIGN;
     const int rs = check_store(dCodes, ldc, dScales, lds, N, 32);
     if (rs != LRBI_OK) return rs;
-    return launch_grad(make_geom(desc), dtype, dDY, lddy, dCodes, ldc, dScales, lds, N, (const uint32_t *)dIp_packed,
-                       (const uint32_t *)dIz_packed, dDW, lddw, (hipStream_t)stream);
+    return launch_checkpoint_grad(make_geom(desc), dtype, dDY, lddy, dCodes, ldc, dScales, lds, N, (const uint32_t *)dIp_packed,
+                                  (const uint32_t *)dIz_packed, dDW, lddw, (hipStream_t)stream);
 }
 
 extern "C" int lrbi_token_logprobs_workspace_bytes(lrbi_dtype dtype, int64_t V, int64_t N, int32_t top, uint64_t *bytes)

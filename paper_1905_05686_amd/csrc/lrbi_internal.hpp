@@ -57,9 +57,8 @@ int launch_f32_gemm(const Geom &g, const float *dW, int64_t ldw, const uint32_t 
                     int64_t ldx, int64_t N, float *dY, int64_t ldy, hipStream_t stream);
 int launch_f32_gemm_t(const Geom &g, lrbi_dtype dt, const void *dW, int64_t ldw, const uint32_t *dIp, const uint32_t *dIz,
                       const void *dDY, int64_t lddy, int64_t N, void *dDX, int64_t lddx, hipStream_t stream);
-// (dXScales: NULL, or the scale bytes of an activation checkpoint whose codes dX are, here and in launch_grad)
-int launch_f32_grad(const Geom &g, const float *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales, int64_t ldxs,
-                    int64_t N, const uint32_t *dIp, const uint32_t *dIz, float *dDW, int64_t lddw, hipStream_t stream);
+int launch_f32_grad(const Geom &g, const float *dDY, int64_t lddy, const float *dX, int64_t ldx, int64_t N,
+                    const uint32_t *dIp, const uint32_t *dIz, float *dDW, int64_t lddw, hipStream_t stream);
 
 // threshold search of Algorithm 1 (lrbi_alg1.hip): workspace layout (byte offsets) and sizes
 struct SearchPlan {
@@ -92,11 +91,12 @@ int pipe_t_slices(const Geom &g, int64_t N, int max_slices, int64_t *iper);
 int launch_pipe_t_gemm(const Geom &g, int slices, int64_t iper, lrbi_dtype dt, const void *dW, int64_t ldw,
                        const uint32_t *dIp, const uint32_t *dIz, const void *dDY, int64_t lddy, int64_t N, void *dDX,
                        int64_t lddx, void *dWorkspace, hipStream_t stream);
-int launch_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales,
-                int64_t ldxs, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream);
+int launch_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx,
+                int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream);
 
 // the weight gradient in 256 x 256 tiles (lrbi_grad256.hip): what it takes, and where it is the better choice
 bool grad256_ok(const Geom &g, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, int64_t N);
+// (dXScales: NULL, or the scale bytes of an activation checkpoint whose codes dX are)
 bool grad256_wins(const Geom &g, int64_t N);
 int launch_grad256(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dX, int64_t ldx, const void *dXScales,
                    int64_t ldxs, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream);
@@ -181,7 +181,9 @@ int launch_quant_unpack(lrbi_dtype dt, const void *dCodes, int64_t ldc, const vo
 int launch_quant_matvec(lrbi_dtype dt, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m, int64_t n,
                         const void *dX, int64_t ldx, int64_t N, void *dY, int64_t ldy, hipStream_t stream);
 
-// activation checkpoints in 8 bits (lrbi_checkpoint.hip)
+// activation checkpoints in 8 bits (lrbi_checkpoint.hip), and the weight gradient from them (lrbi_checkpoint_grad.hip)
+int launch_checkpoint_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dCodes, int64_t ldc, const void *dScales,
+                           int64_t lds, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream);
 int launch_checkpoint_pack(lrbi_dtype dt, const void *dX, int64_t ldx, int64_t n, int64_t N, void *dCodes, int64_t ldc, void *dScales,
                            int64_t lds, hipStream_t stream);
 int launch_checkpoint_unpack(lrbi_dtype dt, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t n, int64_t N,
@@ -279,6 +281,13 @@ inline int compute_units_of(hipStream_t stream)
 // ---------------------------------------------------------------------------
 // Device helpers for Eq. 3 on packed factors.
 // ---------------------------------------------------------------------------
+
+// LDS handed between the lanes of one wavefront: its operations complete in order, the compiler keeps theirs
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 // number of a workgroup in a launch of wide_grid()
 __device__ __forceinline__ int64_t wide_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }

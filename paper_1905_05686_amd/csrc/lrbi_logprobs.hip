@@ -258,12 +258,6 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__re
         for (int p = 0; p < P; ++p) part[(q0 + p) * slices + slice] = make_float4(a[p].m, a[p].s, a[p].t, 0.f);
 }
 
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 static constexpr int LP_LIST = 256;  // words a wavefront holds at a time
 static constexpr int LP_ROUND = 2048; // runs it looks at in a round: eight loads of four a lane, in flight together
 static constexpr int LP_AHEAD = LP_ROUND / 256;
@@ -288,9 +282,9 @@ __device__ __forceinline__ int lp_key_word(uint64_t key) { return (int)~(uint32_
 // number of keys above it; PER keys a lane.
 template <int PER> __device__ __forceinline__ int lp_rank_of(LpList &l, int count, int K, int lane)
 {
-    wave_sync();
+    wave_fence();
     if (lane < 8) l.key[count + lane] = 0; // below every key
-    wave_sync();
+    wave_fence();
     uint64_t k[PER];
     int rank[PER];
 #pragma unroll
@@ -307,11 +301,11 @@ template <int PER> __device__ __forceinline__ int lp_rank_of(LpList &l, int coun
 #pragma unroll
             for (int i = 0; i < PER; ++i) rank[i] += (o[e].x > k[i] ? 1 : 0) + (o[e].y > k[i] ? 1 : 0);
     }
-    wave_sync();
+    wave_fence();
 #pragma unroll
     for (int i = 0; i < PER; ++i)
         if (k[i] && rank[i] < K) l.key[rank[i]] = k[i];
-    wave_sync();
+    wave_fence();
     return count < K ? count : K;
 }
 __device__ __forceinline__ int lp_rank(LpList &l, int count, int K, int lane)
@@ -387,12 +381,12 @@ __device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_
             end += lane >= step ? before : 0;
         }
         const int found = __builtin_amdgcn_readlane(end, 63);
-        wave_sync();
+        wave_fence();
         for (int at = end - __builtin_popcount(hit); hit; hit &= hit - 1) {
             const int bit = __builtin_ctz(hit);
             l.run[at++] = i0 + 256 * (bit >> 2) + 4 * lane + (bit & 3);
         }
-        wave_sync();
+        wave_fence();
         for (int from = 0; from < found; from += 64) {
             const bool in = from + lane < found;
             const int run = l.run[in ? from + lane : from];
@@ -404,9 +398,9 @@ __device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_
             const uint64_t all = __ballot(again);
             const int left = __builtin_popcountll(all);
             if (!left) continue;
-            wave_sync();
+            wave_fence();
             if (again) l.again[__builtin_popcountll(all & below)] = word;
-            wave_sync();
+            wave_fence();
             constexpr int LOADS = 8; // of two runs each, in flight together
             for (int a0 = 0; a0 < left; a0 += 2 * LOADS) {
                 float v[LOADS];
