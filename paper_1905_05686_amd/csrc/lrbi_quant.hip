@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "lrbi_internal.hpp"
+#include "lrbi_mfma_common.hpp"
 #include "lrbi_store.hpp"
 
 namespace lrbi {
@@ -18,102 +19,59 @@ typedef uint32_t q_u32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 q_f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 q_bf16x8 __attribute__((ext_vector_type(8)));
 
-// One lane, one block: 32 weights of a row, 16 bytes of codes, one scale byte.
-template <typename T, bool VEC>
+// A wavefront takes 2048 columns of a row: each lane forms one of their 64 mask words while the weights are on their way, then the
+// lanes go along them eight columns at a time, four lanes a block.
+template <typename T>
 __global__ __launch_bounds__(256) void quant_pack_kernel(Geom g, const T *__restrict__ W, int64_t ldw, const uint32_t *__restrict__ Ip,
                                                          const uint32_t *__restrict__ Iz, unsigned char *__restrict__ codes, int64_t ldc,
-                                                         unsigned char *__restrict__ scales, int64_t lds, int64_t blocks)
+                                                         unsigned char *__restrict__ scales, int64_t lds, int64_t segments)
 {
-    const int64_t at = wide_block() * 256 + threadIdx.x;
-    const int64_t row = at / blocks, b = at - row * blocks;
+    constexpr int COLS = 2048, PIECES = COLS / 512;
+    const int lane = threadIdx.x & 63;
+    const int64_t at = wide_block(), seg = at % segments, row = at / segments * 4 + (threadIdx.x >> 6);
     if (row >= g.m) return;
-    const int64_t j0 = b * STORE_BLOCK;
-    const int left = g.n - j0 < STORE_BLOCK ? (int)(g.n - j0) : STORE_BLOCK;
+    const int64_t j0 = seg * COLS + lane * 8;
     const T *src = W + row * ldw + j0;
-    float v[STORE_BLOCK];
-    if (VEC && left == STORE_BLOCK) {
-        constexpr int PER = 16 / sizeof(T);
+    StorePiece<T> p[PIECES];
 #pragma unroll
-        for (int i = 0; i < STORE_BLOCK / PER; ++i) {
-            const uint4 p = reinterpret_cast<const uint4 *>(src)[i];
-            T e[PER];
-            __builtin_memcpy(e, &p, 16);
-#pragma unroll
-            for (int k = 0; k < PER; ++k) v[i * PER + k] = store_widen(e[k]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < STORE_BLOCK; ++i) v[i] = i < left ? store_widen(src[i]) : 0.f;
-    }
-    uint32_t kept = left == STORE_BLOCK ? 0xFFFFFFFFu : (1u << left) - 1u;
+    for (int i = 0; i < PIECES; ++i) p[i] = store_load<T>(src + 512 * i, g.n - j0 - 512 * i);
+    uint32_t word = 0xFFFFFFFFu;
     if (Ip) {
         const int ti = (int)(row / g.r);
-        kept = decode_word<true>(g, Ip, Iz, ti, (int)(row - (int64_t)ti * g.r), (int)b);
+        word = decode_word<true>(g, Ip, Iz, ti, (int)(row - (int64_t)ti * g.r), (int)(seg * (COLS / 32)) + lane);
     }
-    float most = 0.f;
-    bool finite = true;
 #pragma unroll
-    for (int i = 0; i < STORE_BLOCK; ++i) {
-        if (!((kept >> i) & 1u)) v[i] = 0.f;
-        finite = finite && __builtin_fabsf(v[i]) < __builtin_inff();
-        most = fmaxf(most, __builtin_fabsf(v[i]));
+    for (int i = 0; i < PIECES; ++i) {
+        const uint32_t kept = (uint32_t)__shfl((int)word, 16 * i + (lane >> 2), 64) >> (8 * (lane & 3));
+        if constexpr (sizeof(T) == 2) {
+            p[i].v[0] = apply_mask8(p[i].v[0], kept & 255u);
+        } else {
+            uint32_t w[8];
+            __builtin_memcpy(w, &p[i], 32);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = ((kept >> k) & 1u) ? w[k] : 0u;
+            __builtin_memcpy(&p[i], w, 32);
+        }
+        const uint32_t most = store_most<T>(p[i]);
+        const bool finite = most < StoreBits<T>::inf;
+        const int e = store_exponent<T, 4>(store_magnitude<T>(most));
+        const int64_t j = j0 + 512 * i;
+        if (j - (lane & 3) * 8 >= g.n) continue; // no block here
+        *reinterpret_cast<uint32_t *>(codes + row * ldc + j / 2) = finite ? codes4<T>(p[i], e) : 0u;
+        if ((lane & 3) == 0) scales[row * lds + j / STORE_BLOCK] = finite ? (unsigned char)(e + STORE_BIAS) : 255;
     }
-    const int e = store_exponent<T, 4>(most);
-    const float inv = power_of_two(-e);
-    uint32_t words[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        uint32_t w = 0u;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w |= code4(v[8 * q + k] * inv) << (4 * k);
-        words[q] = finite ? w : 0u;
-    }
-    *reinterpret_cast<uint4 *>(codes + row * ldc + b * 16) = make_uint4(words[0], words[1], words[2], words[3]);
-    scales[row * lds + b] = finite ? (unsigned char)(e + STORE_BIAS) : 255;
 }
 
-// two codes of a 32-bit word, byte B, at their scale
-template <int B> __device__ __forceinline__ uint32_t widen4(__half, uint32_t w, float s)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, B));
-}
-template <int B> __device__ __forceinline__ uint32_t widen4(__hip_bfloat16, uint32_t w, float s)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, B));
-}
-
-// One lane, eight columns.
-template <typename T, bool VEC>
+// A lane takes eight columns.
+template <typename T>
 __global__ __launch_bounds__(256) void quant_unpack_kernel(const unsigned char *__restrict__ codes, int64_t ldc,
                                                            const unsigned char *__restrict__ scales, int64_t lds, int64_t m, int64_t n,
-                                                           T *__restrict__ W, int64_t ldw, int64_t pieces)
+                                                           T *__restrict__ W, int64_t ldw, int64_t pieces, bool is_short)
 {
-    const int64_t at = wide_block() * 256 + threadIdx.x;
-    const int64_t row = at / pieces, p = at - row * pieces;
+    const int64_t at = wide_block() * 256 + threadIdx.x, row = store_row(at, pieces, is_short), p = at - row * pieces;
     if (row >= m) return;
     const uint32_t w = *reinterpret_cast<const uint32_t *>(codes + row * ldc + p * 4);
-    const float s = scale_operand(scales[row * lds + (p >> 2)]);
-    T o[8];
-    if constexpr (sizeof(T) == 4) {
-        f32x2 f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1),
-                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3)};
-        __builtin_memcpy(o, f, 32);
-    } else {
-        uint32_t f[4] = {widen4<0>(T{}, w, s), widen4<1>(T{}, w, s), widen4<2>(T{}, w, s), widen4<3>(T{}, w, s)};
-        __builtin_memcpy(o, f, 16);
-    }
-    T *dst = W + row * ldw + p * 8;
-    if (VEC && p * 8 + 8 <= n) {
-        constexpr int N16 = sizeof(T) * 8 / 16;
-        uint4 q[N16];
-        __builtin_memcpy(q, o, sizeof(o));
-#pragma unroll
-        for (int i = 0; i < N16; ++i) reinterpret_cast<uint4 *>(dst)[i] = q[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (p * 8 + i < n) dst[i] = o[i];
-    }
+    store_values<T>(W + row * ldw + p * 8, values4(T{}, w, scale_operand(scales[row * lds + (p >> 2)])), n - p * 8);
 }
 
 // Y = Wq X.  The codes are read once, straight into registers, and that is what takes the time: 16384 x 16384, one column,
@@ -330,11 +288,9 @@ template <typename T>
 static int launch_pack_t(const Geom &g, const T *W, int64_t ldw, const uint32_t *Ip, const uint32_t *Iz, unsigned char *codes, int64_t ldc,
                          unsigned char *scales, int64_t lds, hipStream_t stream)
 {
-    const int64_t blocks = (g.n + STORE_BLOCK - 1) / STORE_BLOCK, groups = (g.m * blocks + 255) / 256;
+    const int64_t segments = (g.n + 2047) / 2048, groups = (g.m + 3) / 4 * segments;
     if (groups > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    const bool vec = ((uintptr_t)W & 15) == 0 && ldw * (int64_t)sizeof(T) % 16 == 0;
-    auto kern = vec ? quant_pack_kernel<T, true> : quant_pack_kernel<T, false>;
-    LRBI_LAUNCH(kern, wide_grid(groups, 256), dim3(256), 0, stream, g, W, ldw, Ip, Iz, codes, ldc, scales, lds, blocks);
+    LRBI_LAUNCH(quant_pack_kernel<T>, wide_grid(groups, 256), dim3(256), 0, stream, g, W, ldw, Ip, Iz, codes, ldc, scales, lds, segments);
     return LRBI_OK;
 }
 int launch_quant_pack(const Geom &g, lrbi_dtype dt, const void *dW, int64_t ldw, const uint32_t *dIp, const uint32_t *dIz, void *dCodes,
@@ -354,9 +310,8 @@ static int launch_unpack_t(const unsigned char *codes, int64_t ldc, const unsign
 {
     const int64_t pieces = (n + 7) / 8, groups = (m * pieces + 255) / 256;
     if (groups > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    const bool vec = ((uintptr_t)W & 15) == 0 && ldw * (int64_t)sizeof(T) % 16 == 0;
-    auto kern = vec ? quant_unpack_kernel<T, true> : quant_unpack_kernel<T, false>;
-    LRBI_LAUNCH(kern, wide_grid(groups, 256), dim3(256), 0, stream, codes, ldc, scales, lds, m, n, W, ldw, pieces);
+    LRBI_LAUNCH(quant_unpack_kernel<T>, wide_grid(groups, 256), dim3(256), 0, stream, codes, ldc, scales, lds, m, n, W, ldw, pieces,
+                groups * 256 < (int64_t)1 << 32);
     return LRBI_OK;
 }
 int launch_quant_unpack(lrbi_dtype dt, const void *dCodes, int64_t ldc, const void *dScales, int64_t lds, int64_t m, int64_t n, void *dW,

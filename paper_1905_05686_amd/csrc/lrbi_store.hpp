@@ -31,6 +31,10 @@ __device__ __forceinline__ float store_widen(float v) { return v; }
 __device__ __forceinline__ float store_widen(__half v) { return __half2float(v); }
 __device__ __forceinline__ float store_widen(__hip_bfloat16 v) { return __bfloat162float(v); }
 
+__device__ __forceinline__ float store_narrow(float, float v) { return v; }
+__device__ __forceinline__ __half store_narrow(__half, float v) { return __float2half_rn(v); }
+__device__ __forceinline__ __hip_bfloat16 store_narrow(__hip_bfloat16, float v) { return __float2bfloat16(v); }
+
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 // a scale byte as the conversion instructions take it: the exponent field of a 32-bit number (0 stands for 2^-127, 255 for NaN)
@@ -49,25 +53,150 @@ template <typename T, int BITS> __device__ __forceinline__ int store_exponent(fl
     return s < lo ? lo : s > hi ? hi : s;
 }
 
-// the 4-bit code of a value in units of its scale: half steps below 2, whole ones below 4, twos up to 6
-__device__ __forceinline__ uint32_t code4(float v)
+// ---- eight neighbouring values of a row, as they are stored: a lane's share of a block, four lanes a block
+template <typename T> struct StorePiece {
+    uint4 v[sizeof(T) / 2];
+};
+// 16 bytes at any element's address: one instruction, as for an aligned one
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) StoreUnaligned {
+    uint32_t x, y, z, w;
+};
+// `left` values of the row from here on, zeros behind them
+template <typename T> __device__ __forceinline__ StorePiece<T> store_load(const T *src, int64_t left)
 {
-    const float a = __builtin_fabsf(v);
-    const uint32_t low = (uint32_t)(int)__builtin_rintf(a * 2.f);               // 0 .. 4
-    const uint32_t mid = (uint32_t)(int)__builtin_rintf(a) + 2u;                // 4 .. 6
-    uint32_t high = (uint32_t)(int)__builtin_rintf(fminf(a, 6.f) * 0.5f) + 4u;  // 6, 7
-    const uint32_t c = a < 2.f ? low : a < 4.f ? mid : high;
-    return c | ((__builtin_bit_cast(uint32_t, v) >> 28) & 8u);
+    StorePiece<T> p;
+    if (left >= 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const StoreUnaligned<T> u = reinterpret_cast<const StoreUnaligned<T> *>(src)[i];
+            p.v[i] = make_uint4(u.x, u.y, u.z, u.w);
+        }
+    } else {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < left ? src[i] : T{};
+        __builtin_memcpy(&p, e, sizeof(p));
+    }
+    return p;
+}
+template <typename T> __device__ __forceinline__ void store_values(T *dst, const StorePiece<T> &p, int64_t left)
+{
+    if (left >= 8) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<StoreUnaligned<T> *>(dst)[i] = {p.v[i].x, p.v[i].y, p.v[i].z, p.v[i].w};
+    } else {
+        T e[8];
+        __builtin_memcpy(e, &p, sizeof(e));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) dst[i] = e[i];
+    }
+}
+// row and place in it of the `at`-th of rows of `per_row`; short: both below 2^32 (a 64-bit division is ten times the work)
+__device__ __forceinline__ int64_t store_row(int64_t at, int64_t per_row, bool is_short)
+{
+    return is_short ? (int64_t)((uint32_t)at / (uint32_t)per_row) : at / per_row;
+}
+// The largest magnitude of a block as the bits of its number of the type: magnitudes are ordered like their bits, infinities and
+// NaN above every number.
+typedef unsigned short store_u16x2 __attribute__((ext_vector_type(2)));
+template <typename T> __device__ __forceinline__ uint32_t store_most(const StorePiece<T> &p)
+{
+    uint32_t most;
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t w[4] = {p.v[0].x & 0x7FFF7FFFu, p.v[0].y & 0x7FFF7FFFu, p.v[0].z & 0x7FFF7FFFu, p.v[0].w & 0x7FFF7FFFu};
+        const store_u16x2 a = __builtin_elementwise_max(__builtin_bit_cast(store_u16x2, w[0]), __builtin_bit_cast(store_u16x2, w[1]));
+        const store_u16x2 b = __builtin_elementwise_max(__builtin_bit_cast(store_u16x2, w[2]), __builtin_bit_cast(store_u16x2, w[3]));
+        const store_u16x2 c = __builtin_elementwise_max(a, b);
+        most = c.x > c.y ? c.x : c.y;
+    } else {
+        uint32_t w[8];
+        __builtin_memcpy(w, &p, 32);
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = most > (w[i] & 0x7FFFFFFFu) ? most : w[i] & 0x7FFFFFFFu;
+    }
+    const uint32_t one = (uint32_t)__shfl_xor((int)most, 1, 64);
+    most = most > one ? most : one;
+    const uint32_t two = (uint32_t)__shfl_xor((int)most, 2, 64);
+    return most > two ? most : two;
+}
+template <typename T> __device__ __forceinline__ float store_magnitude(uint32_t bits); // of a block's largest
+template <> __device__ __forceinline__ float store_magnitude<float>(uint32_t b) { return __builtin_bit_cast(float, b); }
+template <> __device__ __forceinline__ float store_magnitude<__half>(uint32_t b) { return __half2float(__builtin_bit_cast(__half, (uint16_t)b)); }
+template <> __device__ __forceinline__ float store_magnitude<__hip_bfloat16>(uint32_t b) { return __builtin_bit_cast(float, b << 16); }
+template <typename T> struct StoreBits { // of infinity, and of the magnitude beyond which an 8-bit value is cut
+    static constexpr uint32_t inf = 0x7F800000u, most8 = 0x7F700000u;
+};
+template <> struct StoreBits<__half> {
+    static constexpr uint32_t inf = 0x7C00u, most8 = 0x7B80u;
+};
+template <> struct StoreBits<__hip_bfloat16> {
+    static constexpr uint32_t inf = 0x7F80u, most8 = 0x7F70u;
+};
+
+// The codes of eight values at scale 2^e.  The conversion instructions scale and round (to nearest, ties to even) as the formats
+// ask, checked for every 16-bit number; 4 bits: what rounds past 6 is 6; 8 bits: what rounds past 448 and infinities are NaN.
+typedef __bf16 store_bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 store_f16x2 __attribute__((ext_vector_type(2)));
+typedef short store_s16x2 __attribute__((ext_vector_type(2)));
+template <int B> __device__ __forceinline__ uint32_t narrow4(__half, uint32_t old, uint32_t w, float s)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(old, __builtin_bit_cast(store_f16x2, w), s, B);
+}
+template <int B> __device__ __forceinline__ uint32_t narrow4(__hip_bfloat16, uint32_t old, uint32_t w, float s)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(store_bf16x2, w), s, B);
+}
+template <typename T> __device__ __forceinline__ uint32_t codes4(const StorePiece<T> &p, int e)
+{
+    const float s = power_of_two(e);
+    uint32_t c = 0;
+    if constexpr (sizeof(T) == 2) {
+        c = narrow4<0>(T{}, c, p.v[0].x, s);
+        c = narrow4<1>(T{}, c, p.v[0].y, s);
+        c = narrow4<2>(T{}, c, p.v[0].z, s);
+        c = narrow4<3>(T{}, c, p.v[0].w, s);
+    } else {
+        float f[8];
+        __builtin_memcpy(f, &p, 32);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[0], f[1], s, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[2], f[3], s, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[4], f[5], s, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[6], f[7], s, 3);
+    }
+    return c;
+}
+template <bool HI> __device__ __forceinline__ store_s16x2 narrow8(__half, store_s16x2 old, uint32_t w, float s)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(old, __builtin_bit_cast(store_f16x2, w), s, HI);
+}
+template <bool HI> __device__ __forceinline__ store_s16x2 narrow8(__hip_bfloat16, store_s16x2 old, uint32_t w, float s)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(old, __builtin_bit_cast(store_bf16x2, w), s, HI);
+}
+template <typename T> __device__ __forceinline__ uint2 codes8(const StorePiece<T> &p, int e)
+{
+    const float s = power_of_two(e);
+    store_s16x2 lo = {0, 0}, hi = {0, 0};
+    if constexpr (sizeof(T) == 2) {
+        lo = narrow8<false>(T{}, lo, p.v[0].x, s);
+        lo = narrow8<true>(T{}, lo, p.v[0].y, s);
+        hi = narrow8<false>(T{}, hi, p.v[0].z, s);
+        hi = narrow8<true>(T{}, hi, p.v[0].w, s);
+    } else {
+        float f[8];
+        __builtin_memcpy(f, &p, 32);
+        lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, f[0], f[1], s, false);
+        lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, f[2], f[3], s, true);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, f[4], f[5], s, false);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, f[6], f[7], s, true);
+    }
+    return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 
 // eight 8-bit codes at their scale, exactly
 typedef float store_f32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void widen8(uint2 w, float s, float (&o)[8])
-{
-    const store_f32x2 f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, s, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, s, true),
-                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, s, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, s, true)};
-    __builtin_memcpy(o, f, sizeof(o));
-}
 __device__ __forceinline__ uint4 widen8_f16(uint2 w, float s)
 {
     return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w.x, s, false)),
@@ -82,15 +211,36 @@ __device__ __forceinline__ uint4 widen8_bf16(uint2 w, float s)
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, s, false)),
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, s, true)));
 }
-__device__ __forceinline__ void widen8(uint2 w, float s, __half (&o)[8])
+__device__ __forceinline__ StorePiece<__half> values8(__half, uint2 w, float s) { return {{widen8_f16(w, s)}}; }
+__device__ __forceinline__ StorePiece<__hip_bfloat16> values8(__hip_bfloat16, uint2 w, float s) { return {{widen8_bf16(w, s)}}; }
+__device__ __forceinline__ StorePiece<float> values8(float, uint2 w, float s)
 {
-    const uint4 v = widen8_f16(w, s);
-    __builtin_memcpy(o, &v, sizeof(o));
+    const store_f32x2 f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, s, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, s, true),
+                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, s, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, s, true)};
+    StorePiece<float> p;
+    __builtin_memcpy(&p, f, sizeof(p));
+    return p;
 }
-__device__ __forceinline__ void widen8(uint2 w, float s, __hip_bfloat16 (&o)[8])
+// two 4-bit codes of a 32-bit word, byte B, and all eight of them
+template <int B> __device__ __forceinline__ uint32_t widen4(__half, uint32_t w, float s)
 {
-    const uint4 v = widen8_bf16(w, s);
-    __builtin_memcpy(o, &v, sizeof(o));
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, B));
+}
+template <int B> __device__ __forceinline__ uint32_t widen4(__hip_bfloat16, uint32_t w, float s)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, B));
+}
+template <typename T> __device__ __forceinline__ StorePiece<T> values4(T, uint32_t w, float s)
+{
+    return {{make_uint4(widen4<0>(T{}, w, s), widen4<1>(T{}, w, s), widen4<2>(T{}, w, s), widen4<3>(T{}, w, s))}};
+}
+__device__ __forceinline__ StorePiece<float> values4(float, uint32_t w, float s)
+{
+    const store_f32x2 f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1),
+                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3)};
+    StorePiece<float> p;
+    __builtin_memcpy(&p, f, sizeof(p));
+    return p;
 }
 
 } // namespace lrbi
