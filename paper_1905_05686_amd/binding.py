@@ -194,11 +194,13 @@ def unpack_mask(desc: Desc, mask_bytes: np.ndarray) -> np.ndarray:
 # stream's handle comes without an object around it.
 _codes = None
 _current_stream = None
+_f32 = _i64 = None
 
 
 def _look_up_torch():
-    global _codes, _current_stream
+    global _codes, _current_stream, _f32, _i64
     import torch
+    _f32, _i64 = torch.float32, torch.int64
     raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
     if raw and device:
         _current_stream = lambda: raw(device())  # noqa: E731
@@ -560,32 +562,31 @@ def nmf(desc: Desc, W, Mp, Mz, iters: int, eps: float = 1e-9, method: int = 1, w
     return Mp, Mz
 
 
-def _store(out, rows, cols, block_bytes, device):
-    """Codes and scales of the block formats: the pair given, or new ones with the smallest pitches."""
+def _store(pair, rows, cols, block_bytes):
+    """Addresses and pitches of codes and scales that hold `rows` rows of `cols` values in blocks of 32."""
+    codes, scales = pair
     blocks = -(-cols // 32)
-    if out is None:
-        import torch
-        return (torch.empty((rows, block_bytes * blocks), dtype=torch.uint8, device=device),
-                torch.empty((rows, -(-blocks // 4) * 4), dtype=torch.uint8, device=device))
-    codes, scales = out
-    if codes.shape[0] != rows or scales.shape[0] != rows:
+    if codes.dim() != 2 or scales.dim() != 2 or codes.element_size() != 1 or scales.element_size() != 1:
+        raise ValueError("codes and scales must be matrices of bytes")
+    (crows, ccols), (srows, scols) = codes.shape, scales.shape
+    if crows != rows or srows != rows:
         raise ValueError("codes and scales must have a row for each row")
-    return codes, scales
-
-
-def _bytes(t, what):
-    """Address and row pitch of a matrix of bytes."""
-    if t.element_size() != 1 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be a row-major matrix of bytes" % what)
-    # a tensor of one row may have any stride; its pitch is what it holds
-    return _dev_ptr(t, what), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-def _store_width(codes, scales, cols, block_bytes):
-    """Both hold what `cols` values of a row take."""
-    blocks = -(-cols // 32)
-    if codes.shape[1] < block_bytes * blocks or scales.shape[1] < blocks:
+    if ccols < block_bytes * blocks or scols < blocks:
         raise ValueError("codes or scales have too few columns")
+    (ldc, c1), (lds, s1) = codes.stride(), scales.stride()
+    if c1 != 1 or (s1 != 1 and scols > 1):
+        raise ValueError("codes and scales must be row-major")
+    if rows == 1:  # a single row may have any stride: its pitch is what it holds
+        ldc, lds = ccols // 16 * 16, scols // 4 * 4
+    return _dev_ptr(codes, "codes"), ldc, _dev_ptr(scales, "scales"), lds
+
+
+def _new_store(rows, cols, block_bytes, device):
+    """New codes and scales with the smallest pitches."""
+    import torch
+    blocks = -(-cols // 32)
+    return (torch.empty((rows, block_bytes * blocks), dtype=torch.uint8, device=device),
+            torch.empty((rows, -(-blocks // 4) * 4), dtype=torch.uint8, device=device))
 
 
 def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
@@ -594,13 +595,13 @@ def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
     reuses two tensors.  Returns (codes, scales)."""
     if W.dim() != 2 or W.shape != (desc.m, desc.n) or (desc.n > 1 and W.stride(1) != 1):
         raise ValueError("W must be a row-major [m, n] tensor")
-    codes, scales = _store(out, desc.m, desc.n, 16, W.device)
-    _store_width(codes, scales, desc.n, 16)
-    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    if out is None:
+        out = _new_store(desc.m, desc.n, 16, W.device)
+    cp, ldc, sp, lds = _store(out, desc.m, desc.n, 16)
     _check(load_library().lrbi_quant_pack(
         ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), W.stride(0), None if dIp is None else _dev_ptr(dIp, "Ip"),
         None if dIz is None else _dev_ptr(dIz, "Iz"), cp, ldc, sp, lds, _stream_ptr(stream)), "lrbi_quant_pack")
-    return codes, scales
+    return out
 
 
 def _values_out(out, rows, cols, dtype, device):
@@ -616,9 +617,7 @@ def quant_unpack(codes, scales, n: int, dtype, out=None, stream=None):
     """lrbi_quant_unpack: the values [m, n] of 4-bit codes, as numbers of `dtype`."""
     m = codes.shape[0]
     out = _values_out(out, m, n, dtype, codes.device)
-    _store((codes, scales), m, n, 16, None)
-    _store_width(codes, scales, n, 16)
-    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    cp, ldc, sp, lds = _store((codes, scales), m, n, 16)
     _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _dev_ptr(out, "W"), out.stride(0),
                                             _stream_ptr(stream)), "lrbi_quant_unpack")
     return out
@@ -633,13 +632,10 @@ def quant_matvec(codes, scales, X, out=None, stream=None):
     ldx, x1 = X.stride()
     if N > 1 and x1 != 1:
         raise ValueError("X must be a row-major tensor")
-    if scales.shape[0] != m:
-        raise ValueError("codes and scales must have a row for each row")
-    _store_width(codes, scales, n, 16)
+    cp, ldc, sp, lds = _store((codes, scales), m, n, 16)
     if squeeze and out is not None:
         out = out.unsqueeze(1)
     out, ldy = _row_major_out(out, m, N, X)
-    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
     _check(load_library().lrbi_quant_matvec(_dtype_code(X), cp, ldc, sp, lds, m, n, _dev_ptr(X, "X"), ldx, N, _dev_ptr(out, "Y"), ldy,
                                             _stream_ptr(stream)), "lrbi_quant_matvec")
     return out[:, 0] if squeeze else out
@@ -651,21 +647,19 @@ def checkpoint_pack(X, out=None, stream=None):
     if X.dim() != 2 or (X.shape[1] > 1 and X.stride(1) != 1):
         raise ValueError("X must be a row-major [n, N] tensor")
     n, N = X.shape
-    codes, scales = _store(out, n, N, 32, X.device)
-    _store_width(codes, scales, N, 32)
-    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    if out is None:
+        out = _new_store(n, N, 32, X.device)
+    cp, ldc, sp, lds = _store(out, n, N, 32)
     _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), _dev_ptr(X, "X"), X.stride(0), n, N, cp, ldc, sp, lds,
                                                _stream_ptr(stream)), "lrbi_checkpoint_pack")
-    return codes, scales
+    return out
 
 
 def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
     """lrbi_checkpoint_unpack: the values [n, N] of a checkpoint, as numbers of `dtype`."""
     n = codes.shape[0]
     out = _values_out(out, n, N, dtype, codes.device)
-    _store((codes, scales), n, N, 32, None)
-    _store_width(codes, scales, N, 32)
-    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
+    cp, ldc, sp, lds = _store((codes, scales), n, N, 32)
     _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _dev_ptr(out, "X"), out.stride(0),
                                                  _stream_ptr(stream)), "lrbi_checkpoint_unpack")
     return out
@@ -674,14 +668,13 @@ def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
 def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=None):
     """lrbi_checkpoint_grad: masked_grad with X given as a checkpoint: dW = (dY Xq^T) o decode(Ip, Iz), dY [m, N]."""
     m, n = desc.m, desc.n
-    if dY.dim() != 2 or dY.shape[0] != m or codes.shape[0] != n or scales.shape[0] != n:
+    if dY.dim() != 2 or dY.shape[0] != m:
         raise ValueError("shape mismatch")
     N = dY.shape[1]
     if N > 1 and dY.stride(1) != 1:
         raise ValueError("dY must be a row-major tensor")
-    _store_width(codes, scales, N, 32)
+    cp, ldc, sp, lds = _store((codes, scales), n, N, 32)
     out, lddw = _row_major_out(out, m, n, dY)
-    (cp, ldc), (sp, lds) = _bytes(codes, "codes"), _bytes(scales, "scales")
     _check(load_library().lrbi_checkpoint_grad(
         ctypes.byref(desc), _dtype_code(dY), _dev_ptr(dY, "dY"), dY.stride(0), cp, ldc, sp, lds, N, _dev_ptr(dIp, "Ip"),
         _dev_ptr(dIz, "Iz"), _dev_ptr(out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
@@ -701,17 +694,9 @@ def token_logprobs_workspace_bytes(dtype_code: int, V: int, N: int, top: int = 0
     return out.value
 
 
-def _tokens_ptr(tokens, N):
-    import torch
-    if tokens.dtype != torch.int64 or tokens.shape != (N,) or not tokens.is_contiguous():
-        raise ValueError("tokens must be a contiguous int64 [N] tensor")
-    return _dev_ptr(tokens, "tokens")
-
-
-def _row_ptr(t, shape, what):
-    import torch
-    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous float32 tensor of shape %s" % (what, shape))
+def _row_ptr(t, dtype, shape, what):
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s" % (what, dtype, tuple(shape)))
     return _dev_ptr(t, what)
 
 
@@ -719,28 +704,33 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, 
     """lrbi_token_logprobs: logits [V, N] (row = word, column = token; what masked_gemm returns), tokens int64 [N] (negative:
     padding).  Returns TokenLogprobs; `out` = an earlier call's result of the same shape, which is filled again.  `workspace`:
     device scratch of at least token_logprobs_workspace_bytes bytes (allocated here when None)."""
-    import torch
-    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    if logits.dim() != 2:
         raise ValueError("logits must be a row-major [V, N] tensor")
     V, N = logits.shape
-    dev, code = logits.device, _dtype_code(logits)
+    ldl, inner = logits.stride()
+    if N > 1 and inner != 1:
+        raise ValueError("logits must be a row-major [V, N] tensor")
+    code = _dtype_code(logits)
     if out is None:
-        new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)  # noqa: E731
+        import torch
+        new = lambda *shape: torch.empty(shape, dtype=_f32, device=logits.device)  # noqa: E731
         out = TokenLogprobs(None if tokens is None else new(N), new(N), new(2, N),
-                            torch.empty((top, N), dtype=torch.int64, device=dev) if top > 0 else None, new(top, N) if top > 0 else None)
-    if (out.logp is None) != (tokens is None) or (out.top_ids is None) != (top <= 0):
+                            torch.empty((top, N), dtype=_i64, device=logits.device) if top > 0 else None, new(top, N) if top > 0 else None)
+    logp, entropy, stats, top_ids, top_logp = out
+    if (logp is None) != (tokens is None) or (top_ids is None) != (top <= 0):
         raise ValueError("out is of a call with other results")
     if workspace is None:
-        workspace = torch.empty(token_logprobs_workspace_bytes(code, V, N, top), dtype=torch.uint8, device=dev)
-    if top > 0 and (out.top_ids.shape != (top, N) or out.top_ids.dtype != torch.int64 or not out.top_ids.is_contiguous()):
-        raise ValueError("out.top_ids must be a contiguous int64 [top, N] tensor")
+        import torch
+        workspace = torch.empty(token_logprobs_workspace_bytes(code, V, N, top), dtype=torch.uint8, device=logits.device)
+    row, tok_ptr, logp_ptr, ids_ptr, top_ptr = (N,), None, None, None, None
+    if tokens is not None:
+        tok_ptr, logp_ptr = _row_ptr(tokens, _i64, row, "tokens"), _row_ptr(logp, _f32, row, "out.logp")
+    if top > 0:
+        ids_ptr, top_ptr = _row_ptr(top_ids, _i64, (top, N), "out.top_ids"), _row_ptr(top_logp, _f32, (top, N), "out.top_logp")
     ws_ptr, ws_bytes = _scratch(workspace)
     _check(load_library().lrbi_token_logprobs(
-        code, _dev_ptr(logits, "logits"), logits.stride(0), V, N, None if tokens is None else _tokens_ptr(tokens, N),
-        None if tokens is None else _row_ptr(out.logp, (N,), "out.logp"), _row_ptr(out.entropy, (N,), "out.entropy"),
-        _row_ptr(out.stats, (2, N), "out.stats"), top, _dev_ptr(out.top_ids, "out.top_ids") if top > 0 else None,
-        _row_ptr(out.top_logp, (top, N), "out.top_logp") if top > 0 else None, ws_ptr, ws_bytes, _stream_ptr(stream)),
-        "lrbi_token_logprobs")
+        code, _dev_ptr(logits, "logits"), ldl, V, N, tok_ptr, logp_ptr, _row_ptr(entropy, _f32, row, "out.entropy"),
+        _row_ptr(stats, _f32, (2, N), "out.stats"), top, ids_ptr, top_ptr, ws_ptr, ws_bytes, _stream_ptr(stream)), "lrbi_token_logprobs")
     return out
 
 
@@ -748,13 +738,18 @@ def token_logprobs_grad(logits, tokens, result, g_logp=None, g_entropy=None, out
     """lrbi_token_logprobs_grad: the gradient [V, N] of sum(g_logp * logp + g_entropy * entropy) with respect to the logits,
     from the TokenLogprobs that token_logprobs gave for them.  g_logp, g_entropy: float32 [N], one of them may be None.
     `out` may be `logits` itself."""
-    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    if logits.dim() != 2:
         raise ValueError("logits must be a row-major [V, N] tensor")
     V, N = logits.shape
+    ldl, inner = logits.stride()
+    if N > 1 and inner != 1:
+        raise ValueError("logits must be a row-major [V, N] tensor")
+    code = _dtype_code(logits)
     out, lddl = _row_major_out(out, V, N, logits)
+    row = (N,)
     _check(load_library().lrbi_token_logprobs_grad(
-        _dtype_code(logits), _dev_ptr(logits, "logits"), logits.stride(0), V, N, None if tokens is None else _tokens_ptr(tokens, N),
-        _row_ptr(result.stats, (2, N), "stats"), _row_ptr(result.entropy, (N,), "entropy"),
-        None if g_logp is None else _row_ptr(g_logp, (N,), "g_logp"), None if g_entropy is None else _row_ptr(g_entropy, (N,), "g_entropy"),
+        code, _dev_ptr(logits, "logits"), ldl, V, N, None if tokens is None else _row_ptr(tokens, _i64, row, "tokens"),
+        _row_ptr(result.stats, _f32, (2, N), "stats"), _row_ptr(result.entropy, _f32, row, "entropy"),
+        None if g_logp is None else _row_ptr(g_logp, _f32, row, "g_logp"), None if g_entropy is None else _row_ptr(g_entropy, _f32, row, "g_entropy"),
         _dev_ptr(out, "out"), lddl, _stream_ptr(stream)), "lrbi_token_logprobs_grad")
     return out

@@ -14,7 +14,7 @@
 //
 // Top words.  The rows are cut into runs of 32; the first kernel leaves the largest logit of every run and column, its row, and
 // the second largest.  A word that belongs to the top K lies in a run whose maximum is not below the K-th largest of any K or
-// more such maxima: the finishing wavefront takes the maxima of its 64 lanes' runs and their K-th largest as a bound.  The few
+// more such maxima: the finishing wavefront takes the maxima of its 64 lanes' runs and, to 16 bits, their K-th largest as a bound.  The few
 // runs that reach it give their largest word; only those whose second largest reaches it too are read again.  The words
 // found are ranked by counting.  (Reading every run that reaches the bound: 65536 words, 256 tokens, 20 top words 32 us
 // against 22.)
@@ -341,18 +341,17 @@ __device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_
 #pragma unroll
         for (int k = 0; k < LP_AHEAD; ++k) lp_runs(piece[k], run_max, i0 + 256 * k + 4 * lane, runs);
     }
-    // the K-th largest of the lanes' maxima: fewer than K are above it, K or more are not below it
-    int above = 0, not_below = 0;
+    // a bound that K lanes' maxima reach: the largest number of 16 leading bits for which that holds
+    const uint32_t place = (uint32_t)(lp_key(mine, -1) >> 32);
+    uint32_t leading = 0;
 #pragma unroll
-    for (int j = 0; j < 64; ++j) {
-        const float v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), j));
-        above += v > mine ? 1 : 0;
-        not_below += v >= mine ? 1 : 0;
-    }
-    const float least = __shfl(mine, __builtin_ctzll(__ballot(above < K && not_below >= K)), 64);
+    for (int bit = 31; bit >= 16; --bit)
+        if (__builtin_popcountll(__ballot(place >= (leading | 1u << bit))) >= K) leading |= 1u << bit;
+    const uint64_t least_key = lp_key(none, -1) > (uint64_t)leading << 32 ? lp_key(none, -1) : (uint64_t)leading << 32;
+    const float least = lp_key_logit(least_key);
     // keys that are not above `bound` are behind K others, or of no word
-    const uint64_t lowest = lp_key(none, -1) | 0xFFFFFFFFu, at_least = lp_key(least, -1);
-    uint64_t bound = at_least > lowest ? at_least : lowest;
+    const uint64_t lowest = lp_key(none, -1) | 0xFFFFFFFFu;
+    uint64_t bound = least_key > lowest ? least_key : lowest;
     int count = 0;
     const uint64_t below = (1ull << lane) - 1;
     auto push = [&](uint64_t key, bool in) __attribute__((always_inline)) {
@@ -421,12 +420,44 @@ __device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_
     return lp_rank(l, count, K, lane);
 }
 
+// A column's joined sums: its largest logit and the natural logarithm of its sum, written with what follows from them by lane 0.
+template <typename T>
+__device__ __forceinline__ float lp_write(const LpSums &a, int64_t q, int64_t V, int64_t N, int64_t word, float x, bool has_word,
+                                          float *__restrict__ logp, float *__restrict__ entropy, float *__restrict__ stats, int lane)
+{
+    // the sum was taken at the rounded reference r: brought to the maximum itself
+    const float c = lp_factor<T>(a.m), r = a.m * c, log_s = __log2f(a.s), log_m = log_s - __builtin_fmaf(a.m, c, -r);
+    const float ln_s = LP_LN2 * log_m;
+    if (lane == 0) {
+        const bool empty = a.s == 0.f; // every logit is -infinity
+        stats[q] = empty ? -__builtin_inff() : a.m;
+        stats[N + q] = log_m;
+        if (entropy) entropy[q] = empty ? 0.f : LP_LN2 * (log_s - a.t / a.s);
+        if (has_word) logp[q] = word < 0 ? 0.f : word >= V ? __builtin_nanf("") : empty ? -__builtin_inff() : x - a.m - ln_s;
+    }
+    return ln_s;
+}
+template <typename T> __device__ __forceinline__ LpSums lp_join_lanes(LpSums a, int lanes)
+{
+    for (int step = 1; step < lanes; step *= 2)
+        a = lp_join<T>(a, LpSums{__shfl_xor(a.m, step, 64), __shfl_xor(a.s, step, 64), __shfl_xor(a.t, step, 64)});
+    return a;
+}
+__device__ __forceinline__ void lp_write_top(const LpList &l, int count, const LpSums &a, float ln_s, int64_t q, int64_t N, int K,
+                                             int64_t *__restrict__ top_ids, float *__restrict__ top_logp, int lane)
+{
+    if (lane < K) {
+        top_ids[lane * N + q] = lane < count ? lp_key_word(l.key[lane]) : -1;
+        top_logp[lane * N + q] = lane < count ? lp_key_logit(l.key[lane]) - a.m - ln_s : -__builtin_inff();
+    }
+}
+
 // Joins a column's slices and writes its results, one wavefront a column.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_finish_kernel(
     const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N, const int64_t *__restrict__ tok, const float4 *__restrict__ part,
-    int64_t slices, const float *__restrict__ run_max, const uint32_t *__restrict__ run_more, int64_t run_pitch, float *__restrict__ logp, float *__restrict__ entropy,
-    float *__restrict__ stats, int K, int64_t *__restrict__ top_ids, float *__restrict__ top_logp)
+    int64_t slices, const float *__restrict__ run_max, const uint32_t *__restrict__ run_more, int64_t run_pitch, float *__restrict__ logp,
+    float *__restrict__ entropy, float *__restrict__ stats, int K, int64_t *__restrict__ top_ids, float *__restrict__ top_logp)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t q = wide_block() * (LP_THREADS / 64) + wave;
@@ -452,29 +483,113 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_finish_kernel(
             if (i0 + 64 * k < slices) a = lp_join<T>(a, LpSums{p[k].x, p[k].y, p[k].z});
     }
     const float x = word >= 0 && word < V ? Logit<T>::widen(L[word * ldl + q]) : 0.f;
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2)
-        a = lp_join<T>(a, LpSums{__shfl_xor(a.m, step, 64), __shfl_xor(a.s, step, 64), __shfl_xor(a.t, step, 64)});
-    // the sum was taken at the rounded reference r: brought to the maximum itself
-    const float c = lp_factor<T>(a.m), r = a.m * c, log_s = __log2f(a.s), log_m = log_s - __builtin_fmaf(a.m, c, -r);
-    const float ln_s = LP_LN2 * log_m;
-    if (lane == 0) {
-        const bool empty = a.s == 0.f; // every logit is -infinity
-        stats[q] = empty ? -__builtin_inff() : a.m;
-        stats[N + q] = log_m;
-        if (entropy) entropy[q] = empty ? 0.f : LP_LN2 * (log_s - a.t / a.s);
-        if (logp) logp[q] = word < 0 ? 0.f : word >= V ? __builtin_nanf("") : empty ? -__builtin_inff() : x - a.m - ln_s;
-    }
+    a = lp_join_lanes<T>(a, 64);
+    const float ln_s = lp_write<T>(a, q, V, N, word, x, logp != nullptr, logp, entropy, stats, lane);
     if constexpr (TOP) {
         __shared__ LpList lists[LP_THREADS / 64];
         LpList &l = lists[wave];
         const int count = lp_top(l, L, ldl, (int)V, q, column_runs, run_more + q * run_pitch, runs, piece, K, lane);
-        if (lane < K) {
-            top_ids[lane * N + q] = lane < count ? lp_key_word(l.key[lane]) : -1;
-            top_logp[lane * N + q] = lane < count ? lp_key_logit(l.key[lane]) - a.m - ln_s : -__builtin_inff();
-        }
+        lp_write_top(l, count, a, ln_s, q, N, K, top_ids, top_logp, lane);
     }
 }
+
+// A single column without gaps, up to 32768 words, in one launch: a word of a served sequence.  1024 lanes take eight words at a
+// time, four lanes a run; the runs stay in LDS.  (10000 words f16, 8 top words: 9 us a call against 12 in two launches; 32768 words
+// bf16 10 against 12.4.)
+static constexpr int LP_COLUMN_LANES = 1024;
+static constexpr int LP_COLUMN_SWEEPS = 4;
+static constexpr int LP_COLUMN_MOST = LP_COLUMN_LANES * 8 * LP_COLUMN_SWEEPS;
+template <typename T, bool TOP>
+__global__ __launch_bounds__(LP_COLUMN_LANES) void logprobs_column_kernel(const T *__restrict__ L, int V, const int64_t *__restrict__ tok,
+                                                                          float *__restrict__ logp, float *__restrict__ entropy,
+                                                                          float *__restrict__ stats, int K, int64_t *__restrict__ top_ids,
+                                                                          float *__restrict__ top_logp)
+{
+    __shared__ float4 run_max4[TOP ? LP_COLUMN_MOST / LP_RUN / 4 : 1];
+    __shared__ uint32_t run_more[TOP ? LP_COLUMN_MOST / LP_RUN : 1];
+    __shared__ LpSums join[LP_COLUMN_LANES / 64];
+    float *run_max = (float *)run_max4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float none = -__builtin_inff();
+    const int64_t word = logp ? tok[0] : -1;
+    float x[LP_COLUMN_SWEEPS][8];
+#pragma unroll
+    for (int s = 0; s < LP_COLUMN_SWEEPS; ++s) {
+        const int v0 = (s * LP_COLUMN_LANES + tid) * 8;
+        if (v0 + 8 <= V) {
+            uint4 p[sizeof(T) / 2];
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) p[i] = reinterpret_cast<const uint4 *>(L + v0)[i];
+            T e[8];
+            __builtin_memcpy(e, p, sizeof(e));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[s][i] = Logit<T>::widen(e[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[s][i] = v0 + i < V ? Logit<T>::widen(L[v0 + i]) : none;
+        }
+    }
+    const float own = word >= 0 && word < V ? Logit<T>::widen(L[word]) : 0.f;
+    LpSums a = lp_empty<T>();
+#pragma unroll
+    for (int s = 0; s < LP_COLUMN_SWEEPS; ++s) {
+        if (s * LP_COLUMN_LANES * 8 >= V) break;
+        float b = x[s][0], b2 = none; // largest and second largest
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            b2 = __builtin_amdgcn_fmed3f(x[s][i], b, b2);
+            b = fmaxf(b, x[s][i]);
+        }
+        a.m = fmaxf(a.m, b);
+        if constexpr (TOP) {
+            int row = 0;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) row = x[s][i] == b ? i : row;
+            row += (lane & 3) * 8;
+            b = fmaxf(b, none); // (NaN alone: none)
+#pragma unroll
+            for (int step = 1; step < 4; step *= 2) {
+                const float o = __shfl_xor(b, step, 64), o2 = __shfl_xor(b2, step, 64);
+                const int other = __shfl_xor(row, step, 64);
+                b2 = fmaxf(fmaxf(b2, o2), fminf(b, o));
+                row = o > b || (o == b && other < row) ? other : row;
+                b = fmaxf(b, o);
+            }
+            if ((lane & 3) == 0) {
+                const int run = (s * LP_COLUMN_LANES + tid) / 4;
+                run_max[run] = b;
+                run_more[run] = lp_more(b2, row);
+            }
+        }
+    }
+    const float c = lp_factor<T>(a.m), r = a.m * c;
+#pragma unroll
+    for (int s = 0; s < LP_COLUMN_SWEEPS; ++s) {
+        if (s * LP_COLUMN_LANES * 8 >= V) break;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = __builtin_fmaf(x[s][i], c, -r), e = lp_exp2(d);
+            a.s += e;
+            a.t = __builtin_fmaf(lp_finite(d), e, a.t);
+        }
+    }
+    a = lp_join_lanes<T>(a, 64);
+    if (lane == 0) join[wave] = a;
+    __syncthreads();
+    if (wave > 0) return;
+    a = lp_join_lanes<T>(join[lane & 15], 16);
+    const float ln_s = lp_write<T>(a, 0, V, 1, word, own, logp != nullptr, logp, entropy, stats, lane);
+    if constexpr (TOP) {
+        __shared__ LpList l;
+        const int runs = (V + LP_RUN - 1) / LP_RUN;
+        float piece[LP_AHEAD][4];
+#pragma unroll
+        for (int k = 0; k < LP_AHEAD; ++k) lp_runs(piece[k], run_max, 256 * k + 4 * lane, runs);
+        const int count = lp_top(l, L, 1, V, 0, run_max, run_more, runs, piece, K, lane);
+        lp_write_top(l, count, a, ln_s, 0, 1, K, top_ids, top_logp, lane);
+    }
+}
+static_assert(LP_COLUMN_LANES == 16 * 64 && LP_COLUMN_MOST / LP_RUN <= LP_ROUND, "one partial a lane of 16, one round of runs");
 
 // dx_v = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy); a lane owns P columns and the `batches` batches of 8 rows from
 // ((block * ty_count) + ty) * batches on.
@@ -621,6 +736,12 @@ template <typename T>
 static int launch_logprobs_t(const T *L, int64_t ldl, int64_t V, int64_t N, const int64_t *tok, float *logp, float *entropy,
                              float *stats, int32_t top, int64_t *top_ids, float *top_logp, void *ws, hipStream_t stream)
 {
+    const bool column = N == 1 && ldl == 1 && ((uintptr_t)L & 15) == 0;
+    if (column && V <= LP_COLUMN_MOST) {
+        auto kern = top > 0 ? logprobs_column_kernel<T, true> : logprobs_column_kernel<T, false>;
+        LRBI_LAUNCH(kern, dim3(1), dim3(LP_COLUMN_LANES), 0, stream, L, (int)V, tok, logp, entropy, stats, top, top_ids, top_logp);
+        return LRBI_OK;
+    }
     const LpPlan p = lp_plan((int)sizeof(T), V, N, top, (int64_t)(uintptr_t)L | ldl * (int64_t)sizeof(T));
     float4 *part = (float4 *)ws;
     float *run_max = (float *)((char *)ws + p.part_bytes);
@@ -628,7 +749,6 @@ static int launch_logprobs_t(const T *L, int64_t ldl, int64_t V, int64_t N, cons
     const int threads = p.shape.tx * p.shape.ty <= 64 ? 64 : LP_THREADS, per = LP_THREADS / 64;
     const int64_t blocks = p.shape.col_blocks * p.slices, finish = (N + per - 1) / per;
     if (blocks > 0x7FFFFFFF || finish > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    const bool column = N == 1 && ldl == 1 && ((uintptr_t)L & 15) == 0;
 #define LRBI_PASS_TOP(P, COLUMN, TOP)                                                                                               \
     LRBI_LAUNCH((logprobs_pass_kernel<T, P, COLUMN, TOP>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N, p.shape.tx, \
                 p.shape.ty, p.shape.col_blocks, p.runs, p.slices, part, run_max, run_more, p.run_pitch)
