@@ -683,7 +683,7 @@ def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=No
 
 MAX_TOP = 64
 
-# logp [N] (None without tokens), entropy [N], stats [2, N] float32; top_ids [top, N] int64, top_logp [top, N] float32 (None at top = 0)
+# logp [N] (None without tokens), entropy [N], stats [2, N] float32; top_ids [top, N] int64, top_logp [top, N] float32
 TokenLogprobs = namedtuple("TokenLogprobs", "logp entropy stats top_ids top_logp")
 
 
@@ -712,12 +712,14 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, 
         raise ValueError("logits must be a row-major [V, N] tensor")
     code = _dtype_code(logits)
     if out is None:
+        if top < 0:
+            raise ValueError("top must not be negative")
         import torch
         new = lambda *shape: torch.empty(shape, dtype=_f32, device=logits.device)  # noqa: E731
         out = TokenLogprobs(None if tokens is None else new(N), new(N), new(2, N),
-                            torch.empty((top, N), dtype=_i64, device=logits.device) if top > 0 else None, new(top, N) if top > 0 else None)
+                            torch.empty((top, N), dtype=_i64, device=logits.device), new(top, N))
     logp, entropy, stats, top_ids, top_logp = out
-    if (logp is None) != (tokens is None) or (top_ids is None) != (top <= 0):
+    if (logp is None) != (tokens is None) or top_ids.shape != (top, N):
         raise ValueError("out is of a call with other results")
     if workspace is None:
         import torch

@@ -344,7 +344,8 @@ static int launch_t(const Geom &g, const void *dDY, int64_t lddy, const void *dC
 int launch_checkpoint_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dCodes, int64_t ldc, const void *dScales,
                            int64_t lds, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
 {
-    if (dt != LRBI_F32 && grad256_wins(g, N) && grad256_ok(g, dDY, lddy, dCodes, ldc, N))
+    // (it addresses a block's rows of scales with 32-bit offsets too)
+    if (dt != LRBI_F32 && grad256_wins(g, N) && grad256_ok(g, dDY, lddy, dCodes, ldc, N) && lds < (int64_t)1 << 22)
         return launch_grad256(g, dt, dDY, lddy, dCodes, ldc, dScales, lds, N, dIp, dIz, dDW, lddw, stream);
 #define LRBI_ARGS g, dDY, lddy, dCodes, ldc, dScales, lds, N, dIp, dIz, dDW, lddw, stream
     switch (dt) {

@@ -592,12 +592,12 @@ __global__ __launch_bounds__(LP_COLUMN_LANES) void logprobs_column_kernel(const 
 static_assert(LP_COLUMN_LANES == 16 * 64 && LP_COLUMN_MOST / LP_RUN <= LP_ROUND, "one partial a lane of 16, one round of runs");
 
 // dx_v = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy); a lane owns P columns and the `batches` batches of 8 rows from
-// ((block * ty_count) + ty) * batches on.
+// ((block * ty_count) + ty) * batches on.  DL may be L: a batch is read whole before any of it is written.
 template <typename T, int P>
-__global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N,
+__global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *L, int64_t ldl, int64_t V, int64_t N,
                                                                    const int64_t *__restrict__ tok, const float *__restrict__ stats,
                                                                    const float *__restrict__ entropy, const float *__restrict__ g_logp,
-                                                                   const float *__restrict__ g_entropy, T *__restrict__ DL, int64_t lddl,
+                                                                   const float *__restrict__ g_entropy, T *DL, int64_t lddl,
                                                                    int tx_count, int ty_count, int64_t col_blocks, int64_t batches)
 {
     __shared__ float column[7][64 * P]; // factor, reference, log2 of the sum, the two gradients, entropy, word of every column
@@ -675,29 +675,29 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *__re
 }
 
 // Columns per lane and lanes per row.  A piece of P columns is one load: P divides N and the row pitch, the base is aligned to
-// it.  Wider pieces need fewer instructions a column, and fewer lanes: they are taken while every SIMD still gets two
-// wavefronts of lanes with `rows` rows each.
+// it.  Wider pieces need fewer instructions a column, and fewer lanes: they are taken while `lanes` of them with `rows` rows each
+// are left (131072: two wavefronts on every SIMD).
 struct LpShape {
     int p, tx, ty;
     int64_t col_blocks;
 };
-static LpShape lp_shape(int es, int64_t V, int64_t N, int64_t bits, int rows, int most_bytes)
+static LpShape lp_shape(int es, int64_t V, int64_t N, int64_t bits, int rows, int most_bytes, int least, int64_t lanes)
 {
     LpShape s;
     s.p = 1;
     const int64_t pieces_of_rows = (V + rows - 1) / rows;
     for (int p = most_bytes / es; p > 1; p /= 2) {
         if (N % p != 0 || (bits & (p * es - 1)) != 0) continue;
-        if (p > 2 && pieces_of_rows * (N / p) < 131072) continue;
+        if (p > least && pieces_of_rows * (N / p) < lanes) continue;
         s.p = p;
         break;
     }
     const int64_t pieces = N / s.p;
     // few lanes in all: workgroups of one wavefront, so that more compute units take part
     const int threads = pieces_of_rows * pieces <= 16384 ? 64 : LP_THREADS;
-    s.tx = pieces < 64 ? (int)pieces : 64;
+    s.col_blocks = (pieces + 63) / 64;
+    s.tx = (int)((pieces + s.col_blocks - 1) / s.col_blocks); // (300 columns in 75 pieces: 38 and 37 lanes, not 64 and 11)
     s.ty = threads / s.tx;
-    s.col_blocks = (pieces + s.tx - 1) / s.tx;
     return s;
 }
 
@@ -710,7 +710,9 @@ struct LpPlan {
 static LpPlan lp_plan(int es, int64_t V, int64_t N, int32_t top, int64_t bits)
 {
     LpPlan p;
-    p.shape = lp_shape(es, V, N, bits, LP_RUN, 8);
+    // The top words' comparisons are hidden by more wavefronts (65536 words, 256 tokens bf16: 8-byte pieces 24.6 us, 2-byte ones
+    // 22.5; 131072 words, 64 tokens 22.1 and 22.8).
+    p.shape = top > 0 ? lp_shape(es, V, N, bits, LP_RUN, 8, 1, 524288) : lp_shape(es, V, N, bits, LP_RUN, 8, 2, 131072);
     const int64_t all = (V + LP_RUN - 1) / LP_RUN;
     // runs a lane: as many as leave 2048 workgroups, eight for each compute unit
     const int64_t groups = (all + p.shape.ty - 1) / p.shape.ty * p.shape.col_blocks;
@@ -795,7 +797,7 @@ static int launch_logprobs_grad_t(const T *L, int64_t ldl, int64_t V, int64_t N,
                                   hipStream_t stream)
 {
     const int64_t bits = (int64_t)((uintptr_t)L | (uintptr_t)DL) | (ldl | lddl) * (int64_t)sizeof(T);
-    const LpShape s = lp_shape((int)sizeof(T), V, N, bits, LP_GRAD, 16);
+    const LpShape s = lp_shape((int)sizeof(T), V, N, bits, LP_GRAD, 16, 2, 131072);
     const int threads = s.tx * s.ty <= 64 ? 64 : LP_THREADS;
     // batches a lane, for whose columns it reads 28 bytes each: up to eight while 2048 workgroups are left
     int64_t batches = (V + LP_GRAD - 1) / LP_GRAD / s.ty * s.col_blocks / 2048;

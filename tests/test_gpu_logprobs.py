@@ -46,7 +46,7 @@ def _check(logits, tokens, top, dtype, result=None):
         want = np.where(ids < 0, -np.inf, np.take_along_axis(lp, np.maximum(ids, 0), axis=0))
         _near(to_float64(r.top_logp), want, lse_tol + 2.0 ** -22 * np.where(np.isfinite(want), np.abs(want), 0))
     else:
-        assert r.top_ids is None
+        assert r.top_ids.shape == (0, N) and r.top_logp.shape == (0, N)
     stats = to_float64(r.stats)
     fine = np.isfinite(x).any(axis=0) & ~np.isnan(lp).any(axis=0)
     with np.errstate(invalid="ignore"):

@@ -110,6 +110,7 @@ def test_binding_refuses_wrong_tensors():
                  lambda: lrbi.token_logprobs(torch.zeros(5)), lambda: lrbi.token_logprobs(torch.zeros(5, 6).t()),
                  lambda: lrbi.token_logprobs(torch.zeros(5, 6), torch.zeros(5, dtype=torch.int64)),
                  lambda: lrbi.token_logprobs(torch.zeros(5, 6), torch.zeros(6, dtype=torch.int32)),
-                 lambda: lrbi.token_logprobs(torch.zeros(5, 6), out=lrbi.TokenLogprobs(torch.zeros(6), *[None] * 4))):
+                 lambda: lrbi.token_logprobs(torch.zeros(5, 6), out=lrbi.TokenLogprobs(torch.zeros(6), *[torch.zeros(6)] * 4)),
+                 lambda: lrbi.token_logprobs(torch.zeros(5, 6), top=-1)):
         with pytest.raises(ValueError):
             call()
