@@ -53,37 +53,122 @@ __device__ __forceinline__ uint4 cg_widen(BF16Tag, uint2 w, float s) { return wi
 __device__ __forceinline__ uint16_t cg_narrow(F16Tag, float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 __device__ __forceinline__ uint16_t cg_narrow(BF16Tag, float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 
-// 16 bytes of a row at any element's address, columns q on: zeros from column N on.  A piece that the row's end cuts off is read as
-// the row's last 16 bytes and moved down.
-template <typename E> __device__ __forceinline__ uint4 cg_load(const E *row, int q, int N, bool whole)
+// 16 bytes of a row at any element's address, columns q on.  What lies behind column N is zero once cg_trim has seen it: a piece that the
+// row's end cuts off is read as the row's last 16 bytes and moved down, when it is staged (at the load it would be waited for).
+template <typename E> __device__ __forceinline__ uint4 cg_load(const E *row, int q, int N)
 {
     constexpr int U = 16 / sizeof(E);
     struct __attribute__((packed, aligned(sizeof(E)))) Piece {
-        uint64_t lo, hi;
+        uint32_t x, y, z, w;
     };
-    uint64_t lo = 0, hi = 0;
     if (N >= U) {
-        const int from = q < N - U ? q : N - U;
-        const Piece p = *reinterpret_cast<const Piece *>(row + from);
-        lo = p.lo;
-        hi = p.hi;
-        if (!whole) {
-            const int s = (q - from) * (int)sizeof(E) * 8; // bits
-            lo = s >= 64 ? hi >> (s & 63) : s ? lo >> s | hi << (64 - s) : lo;
-            hi = s >= 64 ? 0 : hi >> s;
-            if (s >= 128) lo = 0;
-        }
-    } else {
+        const Piece p = *reinterpret_cast<const Piece *>(row + (q < N - U ? q : N - U));
+        return make_uint4(p.x, p.y, p.z, p.w);
+    }
+    uint64_t lo = 0, hi = 0; // a row of less than 16 bytes
 #pragma unroll 1
-        for (int e = 0; e < U && q + e < N; ++e) {
-            uint64_t v = 0;
-            __builtin_memcpy(&v, row + q + e, sizeof(E));
-            const int s = e * (int)sizeof(E) * 8;
-            if (s < 64) lo |= v << s;
-            else hi |= v << (s - 64);
-        }
+    for (int e = 0; e < U && q + e < N; ++e) {
+        uint64_t v = 0;
+        __builtin_memcpy(&v, row + q + e, sizeof(E));
+        const int s = e * (int)sizeof(E) * 8;
+        if (s < 64) lo |= v << s;
+        else hi |= v << (s - 64);
     }
     return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+template <typename E> __device__ __forceinline__ uint4 cg_trim(uint4 v, int q, int N)
+{
+    constexpr int U = 16 / sizeof(E);
+    const int over = q - (N - U);
+    if (N < U || over <= 0) return v;
+    const int s = (over < U ? over : U) * (int)sizeof(E) * 8; // bits
+    uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+    lo = s >= 128 ? 0 : s >= 64 ? hi >> (s & 63) : lo >> s | hi << (64 - s);
+    hi = s >= 64 ? 0 : hi >> s;
+    return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
+// 16 codes from column p on, zeros behind column N: p of a piece behind the last one that exists is read as that one
+__device__ __forceinline__ int cg_piece(int p, int N) { return p < N ? p : (N - 1) & ~15; }
+__device__ __forceinline__ uint4 cg_trim_codes(uint4 v, int p, int N)
+{
+    const int left = N - p; // codes that count
+    if (left >= 16) return v;
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = left >= 4 * k + 4 ? w[k] : left <= 4 * k ? 0u : w[k] & ((1u << (8 * (left - 4 * k))) - 1u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Eight fp32 numbers as three bf16 parts each: cut off, not rounded, 8 of the 24 bits each; an infinity or a NaN is its first part
+// alone.
+__device__ __forceinline__ void cg_split(const uint4 (&y)[2], uint4 (&parts)[3])
+{
+    uint32_t y8[8], h[3][4];
+    __builtin_memcpy(y8, y, 32);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t e3[3][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t u = y8[2 * k + e];
+            const bool finite = __builtin_isfinite(__builtin_bit_cast(float, u));
+            const float v = finite ? __builtin_bit_cast(float, u) - __builtin_bit_cast(float, u & 0xFFFF0000u) : 0.f;
+            e3[0][e] = u;
+            if (__builtin_isnan(__builtin_bit_cast(float, u))) e3[0][e] = 0x7FFF0000u; // (its bits may lie below the cut)
+            e3[1][e] = __builtin_bit_cast(uint32_t, v);
+            e3[2][e] = __builtin_bit_cast(uint32_t, v - __builtin_bit_cast(float, e3[1][e] & 0xFFFF0000u));
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) h[q][k] = __builtin_amdgcn_perm(e3[q][1], e3[q][0], 0x07060302u); // the upper halves
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) parts[q] = make_uint4(h[q][0], h[q][1], h[q][2], h[q][3]);
+}
+
+// What a wavefront needs for the mask words of 64 x 64 entries from (i0, j0) on, one row a lane: slices of the factors, asked for before
+// the products, or the words themselves.  lined_up: tile sizes are multiples of 64, ranks up to 64 (a tile that the matrix cuts off
+// has whole factors; what lies outside is not stored).
+struct CgMask {
+    uint32_t z[2], p[2], words[2];
+};
+__device__ __forceinline__ CgMask cg_mask_begin(const Geom &g, const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz, int64_t i0,
+                                                int64_t j0, bool lined_up, int lane)
+{
+    CgMask q = {{0u, 0u}, {0u, 0u}, {0u, 0u}};
+    if (i0 >= g.m || j0 >= g.n) return q;
+    if (lined_up) {
+        const int ti = (int)(i0 / g.r), tj = (int)(j0 / g.c);
+        const int64_t t = (int64_t)ti * g.tile_cols + tj;
+        const int il = (int)(i0 - (int64_t)ti * g.r) + lane, zw = (int)((j0 - (int64_t)tj * g.c) >> 5);
+        if (lane < g.k) {
+            const u32x2 v = *reinterpret_cast<const u32x2 *>(Iz + (t * g.k + lane) * g.izw + zw);
+            q.z[0] = v.x;
+            q.z[1] = v.y;
+        }
+        q.p[0] = Ip[(t * g.r + il) * g.ipw];
+        if (g.ipw > 1) q.p[1] = Ip[(t * g.r + il) * g.ipw + 1];
+    } else if (i0 + lane < g.m) {
+        const int ti = (int)((i0 + lane) / g.r), il = (int)(i0 + lane - (int64_t)ti * g.r);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) q.words[w] = decode_word<true>(g, Ip, Iz, ti, il, (int)(j0 >> 5) + w);
+    }
+    return q;
+}
+// fz: 64 pairs of words of the wavefront's own
+__device__ __forceinline__ void cg_mask_end(CgMask &q, uint32_t *fz, bool lined_up, int lane)
+{
+    if (!lined_up) return;
+    wave_fence();
+    *reinterpret_cast<u32x2 *>(fz + lane * 2) = u32x2{q.z[0], q.z[1]};
+    wave_fence();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        for (uint32_t sel = q.p[h]; sel; sel &= sel - 1u) {
+            const u32x2 v = *reinterpret_cast<const u32x2 *>(fz + (__builtin_ctz(sel) + 32 * h) * 2);
+            q.words[0] |= v.x;
+            q.words[1] |= v.y;
+        }
 }
 
 template <typename Tag>
@@ -92,7 +177,7 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
                                                                      const unsigned char *__restrict__ XS, int64_t ldxs, int N,
                                                                      const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz,
                                                                      typename CgTypes<Tag>::elem *__restrict__ DW, int64_t lddw,
-                                                                     int64_t jblocks, int64_t blocks, int w_vec_ok)
+                                                                     int64_t jblocks, int64_t blocks)
 {
     typedef typename CgTypes<Tag>::elem E;
     typedef typename CgTypes<Tag>::op Op;
@@ -111,68 +196,52 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
     constexpr int AV = sizeof(E) / 2; // 16-byte pieces of eight elements
     uint4 areg[4][AV];
     uint4 xreg[2];
-    uint32_t sreg; // two bytes
+    uint32_t sreg[2];
     auto load = [&](int64_t block, int slab) __attribute__((always_inline)) {
         const int64_t ib = block / jblocks, i0 = ib * CG_B, j0 = (block - ib * jblocks) * CG_B;
         const int q = slab * CG_K + (tid & 7) * 8;
-        const bool whole = (slab + 1) * CG_K <= N;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int64_t i = i0 + (tid >> 3) + 32 * c, row = i < g.m ? i : g.m - 1; // (rows past the matrix are not stored)
 #pragma unroll
-            for (int k = 0; k < AV; ++k) areg[c][k] = cg_load(DY + row * lddy, q + k * (16 / (int)sizeof(E)), N, whole);
+            for (int k = 0; k < AV; ++k) areg[c][k] = cg_load(DY + row * lddy, q + k * (16 / (int)sizeof(E)), N);
         }
-        const int p = slab * CG_K + (tid & 3) * 16;
-        sreg = 0;
+        const int p = cg_piece(slab * CG_K + (tid & 3) * 16, N);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int64_t j = j0 + (tid >> 2) + 64 * c, row = j < g.n ? j : g.n - 1;
-            xreg[c] = make_uint4(0u, 0u, 0u, 0u);
-            if (p < N) { // a block is whole, zeros behind column N
-                xreg[c] = *reinterpret_cast<const uint4 *>(X + row * ldx + p);
-                sreg |= (uint32_t)XS[row * ldxs + (p >> 5)] << (8 * c);
-            }
+            xreg[c] = *reinterpret_cast<const uint4 *>(X + row * ldx + p);
+            sreg[c] = XS[row * ldxs + (p >> 5)];
         }
     };
-    auto stage = [&]() __attribute__((always_inline)) {
+    auto stage = [&](int slab) __attribute__((always_inline)) {
+        if ((slab + 1) * CG_K > N) { // the last slab: columns behind N are zero
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int k = 0; k < AV; ++k)
+                    areg[c][k] = cg_trim<E>(areg[c][k], slab * CG_K + (tid & 7) * 8 + k * (16 / (int)sizeof(E)), N);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) xreg[c] = cg_trim_codes(xreg[c], slab * CG_K + (tid & 3) * 16, N);
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             unsigned char *dst = smem + ((tid >> 3) + 32 * c) * (CG_A_ROW * 2) + (tid & 7) * 16;
             if constexpr (PARTS == 1) {
                 *reinterpret_cast<uint4 *>(dst) = areg[c][0];
             } else {
-                uint32_t parts[3][4], y8[8];
-                __builtin_memcpy(y8, areg[c], 32);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    // cut off, not rounded: 8 of the 24 bits each; an infinity or a NaN is its first part alone
-                    uint32_t h[3][2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint32_t u = y8[2 * k + e];
-                        float y = __builtin_bit_cast(float, u);
-                        const bool finite = __builtin_fabsf(y) < __builtin_inff();
-                        if (!finite) u |= (u & 0x7FFFFFu) ? 0x400000u : 0u;
-                        h[0][e] = u >> 16;
-                        y -= __builtin_bit_cast(float, u & 0xFFFF0000u);
-                        u = finite ? __builtin_bit_cast(uint32_t, y) : 0u;
-                        h[1][e] = u >> 16;
-                        y -= __builtin_bit_cast(float, u & 0xFFFF0000u);
-                        h[2][e] = finite ? __builtin_bit_cast(uint32_t, y) >> 16 : 0u;
-                    }
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) parts[q][k] = h[q][0] | h[q][1] << 16;
-                }
+                uint4 parts[3];
+                cg_split(areg[c], parts);
 #pragma unroll
                 for (int q = 0; q < 3; ++q)
-                    *reinterpret_cast<uint4 *>(dst + q * S::a_bytes) = make_uint4(parts[q][0], parts[q][1], parts[q][2], parts[q][3]);
+                    *reinterpret_cast<uint4 *>(dst + q * S::a_bytes) = parts[q];
             }
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int row = (tid >> 2) + 64 * c;
             *reinterpret_cast<uint4 *>(smem + S::x_off + row * CG_X_ROW + (tid & 3) * 16) = xreg[c];
-            if ((tid & 1) == 0) *reinterpret_cast<uint32_t *>(smem + S::s_off + row * 8 + ((tid >> 1) & 1) * 4) = (sreg >> (8 * c) & 255u) << 23;
+            if ((tid & 1) == 0) *reinterpret_cast<uint32_t *>(smem + S::s_off + row * 8 + ((tid >> 1) & 1) * 4) = sreg[c] << 23;
         }
     };
 
@@ -184,26 +253,7 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
         const int64_t ib = block / jblocks;
         // this wavefront's 64 x 64
         const int64_t i0 = ib * CG_B + wi * 64, j0 = (block - ib * jblocks) * CG_B + wj * 64;
-        // ---- factors under it, or its mask words: lane = row
-        uint32_t z[2] = {0u, 0u}, p[2] = {0u, 0u}, words[2] = {0u, 0u};
-        if (i0 < g.m && j0 < g.n) {
-            if (lined_up) { // (a tile that the matrix cuts off has whole factors; what lies outside is not stored)
-                const int ti = (int)(i0 / g.r), tj = (int)(j0 / g.c);
-                const int64_t t = (int64_t)ti * g.tile_cols + tj;
-                const int il = (int)(i0 - (int64_t)ti * g.r) + lane, zw = (int)((j0 - (int64_t)tj * g.c) >> 5);
-                if (lane < g.k) {
-                    const u32x2 v = *reinterpret_cast<const u32x2 *>(Iz + (t * g.k + lane) * g.izw + zw);
-                    z[0] = v.x;
-                    z[1] = v.y;
-                }
-                p[0] = Ip[(t * g.r + il) * g.ipw];
-                if (g.ipw > 1) p[1] = Ip[(t * g.r + il) * g.ipw + 1];
-            } else if (i0 + lane < g.m) {
-                const int ti = (int)((i0 + lane) / g.r), il = (int)(i0 + lane - (int64_t)ti * g.r);
-#pragma unroll
-                for (int w = 0; w < 2; ++w) words[w] = decode_word<true>(g, Ip, Iz, ti, il, (int)(j0 >> 5) + w);
-            }
-        }
+        CgMask q = cg_mask_begin(g, Ip, Iz, i0, j0, lined_up, lane);
         // ---- products
         f32x16 acc[2][2];
 #pragma unroll
@@ -215,7 +265,7 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
 #pragma unroll 1
         for (int s = 0; s < nslabs; ++s) {
             __syncthreads(); // the slab before has been read
-            stage();
+            stage(s);
             const bool more = s + 1 < nslabs;
             if (more || next < blocks) load(more ? block : next, more ? s + 1 : 0);
             __syncthreads();
@@ -239,27 +289,19 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
 #pragma unroll
                     for (int a = 0; a < 2; ++a)
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) acc[a][b] = mfma_32x32x16(Op{}, xf[a], yf[b], acc[a][b]);
+                        for (int b = 0; b < 2; ++b)
+                            acc[a][b] = PARTS == 1 ? mfma_32x32x16(Op{}, xf[a], yf[b], acc[a][b]) : mfma_32x32x16(Op{}, yf[b], xf[a], acc[a][b]);
                 }
             }
         }
-        // ---- mask words of row `lane`
-        if (lined_up) {
-            wave_fence();
-            *reinterpret_cast<u32x2 *>(fz + lane * 2) = u32x2{z[0], z[1]};
-            wave_fence();
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                for (uint32_t sel = p[h]; sel; sel &= sel - 1u) {
-                    const u32x2 v = *reinterpret_cast<const u32x2 *>(fz + (__builtin_ctz(sel) + 32 * h) * 2);
-                    words[0] |= v.x;
-                    words[1] |= v.y;
-                }
-        }
-        // ---- masked output: per 32 x 32 block the lane holds row l32 (of dW) and columns 8 * (v / 4) + 4 * lg + (v % 4)
-        if constexpr (PARTS == 1) {
+        cg_mask_end(q, fz, lined_up, lane);
+        const uint32_t (&words)[2] = q.words;
+        // ---- masked output
+        if constexpr (PARTS == 1) { // per 32 x 32 block the lane holds row l32 (of dW) and columns 8 * (v / 4) + 4 * lg + (v % 4)
             wave_fence();
             *reinterpret_cast<u32x2 *>(mask + lane * 2) = u32x2{words[0], words[1]};
+            int ln = lane; // what is derived from it here is not to occupy registers during the products
+            asm volatile("" : "+v"(ln));
             uint16_t *strip = (uint16_t *)(smem + S::c_off) + wave * (32 * CG_C_ROW);
             const unsigned char *mb = (const unsigned char *)mask;
 #pragma unroll
@@ -278,16 +320,19 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
                     }
                 wave_fence();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) { // eight rows an instruction, 128 bytes each
-                    const int rr = 8 * q + (lane >> 3), pc = lane & 7;
+                for (int v8 = 0; v8 < 4; ++v8) { // eight rows an instruction, 128 bytes each
+                    const int rr = 8 * v8 + (ln >> 3), pc = ln & 7;
                     const uint2 lo = *reinterpret_cast<const uint2 *>(strip + rr * CG_C_ROW + pc * 8);
                     const uint2 hi = *reinterpret_cast<const uint2 *>(strip + rr * CG_C_ROW + pc * 8 + 4);
                     const uint4 v = apply_mask8(make_uint4(lo.x, lo.y, hi.x, hi.y), (uint32_t)mb[(b * 32 + rr) * 8 + pc]);
                     const int64_t i = i0 + b * 32 + rr, j = j0 + pc * 8;
                     if (i >= g.m || j >= g.n) continue;
                     E *dst = DW + i * lddw + j;
-                    if (w_vec_ok && j + 8 <= g.n) {
-                        *reinterpret_cast<uint4 *>(dst) = v;
+                    if (j + 8 <= g.n) {
+                        struct __attribute__((packed, aligned(2))) Piece { // at any element's address
+                            uint32_t x, y, z, w;
+                        };
+                        *reinterpret_cast<Piece *>(dst) = {v.x, v.y, v.z, v.w};
                     } else {
                         const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -296,32 +341,201 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
                     }
                 }
             }
-        } else {
+        } else { // the lane holds column l32 and rows 8 * (v / 4) + 4 * lg + (v % 4): a store is two rows of 128 bytes
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int64_t i = i0 + b * 32 + l32;
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int a = 0; a < 2; ++a) {
-                    const uint32_t word = __shfl(words[a], b * 32 + l32, 64);
+                for (int v = 0; v < 16; ++v) {
+                    const int rr = b * 32 + 8 * (v >> 2) + (v & 3);
+                    const int64_t i = i0 + rr + 4 * lg;
+                    if (i >= g.m) continue;
+                    E *dst = DW + i * lddw + j0 + l32;
 #pragma unroll
-                    for (int v4 = 0; v4 < 4; ++v4) {
-                        float o[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = ((word >> (8 * v4 + 4 * lg + e)) & 1u) ? acc[a][b][4 * v4 + e] : 0.f;
-                        const int64_t j = j0 + a * 32 + 8 * v4 + 4 * lg;
-                        if (i >= g.m || j >= g.n) continue;
-                        E *dst = DW + i * lddw + j;
-                        if (w_vec_ok && j + 4 <= g.n) {
-                            *reinterpret_cast<float4 *>(dst) = make_float4(o[0], o[1], o[2], o[3]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (j + e < g.n) dst[e] = o[e];
-                        }
+                    for (int a = 0; a < 2; ++a) {
+                        const uint32_t lo = __builtin_amdgcn_readlane(words[a], rr), hi = __builtin_amdgcn_readlane(words[a], rr + 4);
+                        if (j0 + a * 32 + l32 < g.n) dst[a * 32] = ((lg ? hi : lo) >> l32 & 1u) ? acc[a][b][v] : 0.f;
                     }
                 }
+        }
+    }
+}
+
+// The same for few blocks: 64 x 64 of dW a workgroup, slabs of 128 batch columns, a quarter of which each wavefront multiplies; the
+// four sums are added in LDS.
+static constexpr int CS_B = 64, CS_K = 128;
+static constexpr int CS_A_ROW = CS_K + 8;  // halfs
+static constexpr int CS_X_ROW = CS_K + 16; // bytes
+static constexpr int CS_P_ROW = CS_B + 4;  // floats of a row of partial sums
+template <typename Tag> struct SmemCs {
+    static constexpr int a_bytes = CS_B * CS_A_ROW * 2;
+    static constexpr int x_off = CgTypes<Tag>::parts * a_bytes;
+    static constexpr int s_off = x_off + CS_B * CS_X_ROW; // [64 rows][4 blocks]
+    static constexpr int staged = s_off + CS_B * 4 * 4;
+    static constexpr int sums = 4 * CS_B * CS_P_ROW * 4; // in their place, behind the last slab
+    static constexpr int w_off = staged > sums ? staged : sums; // factor slice [64][2], mask words [64][2]
+    static constexpr int bytes = w_off + 2 * 64 * 8;
+};
+
+template <typename Tag>
+__global__ __launch_bounds__(CG_THREADS, 2) void checkpoint_grad_small_kernel(Geom g, const typename CgTypes<Tag>::elem *__restrict__ DY,
+                                                                              int64_t lddy, const unsigned char *__restrict__ X, int64_t ldx,
+                                                                              const unsigned char *__restrict__ XS, int64_t ldxs, int N,
+                                                                              const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz,
+                                                                              typename CgTypes<Tag>::elem *__restrict__ DW, int64_t lddw,
+                                                                              int64_t jblocks)
+{
+    typedef typename CgTypes<Tag>::elem E;
+    typedef typename CgTypes<Tag>::op Op;
+    constexpr int PARTS = CgTypes<Tag>::parts;
+    using S = SmemCs<Tag>;
+    extern __shared__ uint4 lrbi_dyn_smem[];
+    unsigned char *smem = (unsigned char *)lrbi_dyn_smem;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, lg = lane >> 5;
+    const int64_t ib = blockIdx.x / jblocks, i0 = ib * CS_B, j0 = (blockIdx.x - ib * jblocks) * CS_B;
+    const int nslabs = (N + CS_K - 1) / CS_K;
+    const bool lined_up = g.c % 64 == 0 && g.r % 64 == 0 && g.k <= FAST_MAX_K;
+
+    // lane = (row tid / 16 + 16 c, eight columns tid % 16) of dY, (row tid / 8 + 32 c, 16 columns tid % 8) of X
+    constexpr int AV = sizeof(E) / 2;
+    uint4 areg[4][AV], xreg[2];
+    uint32_t sreg[2];
+    auto load = [&](int slab) __attribute__((always_inline)) {
+        const int q = slab * CS_K + (tid & 15) * 8;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int64_t i = i0 + (tid >> 4) + 16 * c, row = i < g.m ? i : g.m - 1; // (rows past the matrix are not stored)
+#pragma unroll
+            for (int k = 0; k < AV; ++k) areg[c][k] = cg_load(DY + row * lddy, q + k * (16 / (int)sizeof(E)), N);
+        }
+        const int p = cg_piece(slab * CS_K + (tid & 7) * 16, N);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int64_t j = j0 + (tid >> 3) + 32 * c, row = j < g.n ? j : g.n - 1;
+            xreg[c] = *reinterpret_cast<const uint4 *>(X + row * ldx + p);
+            sreg[c] = XS[row * ldxs + (p >> 5)];
+        }
+    };
+    load(0);
+    CgMask q = {};
+    if (wave == 0) q = cg_mask_begin(g, Ip, Iz, i0, j0, lined_up, lane);
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
+#pragma unroll 1
+    for (int s = 0; s < nslabs; ++s) {
+        if (s) __syncthreads(); // the slab before has been read
+        if ((s + 1) * CS_K > N) { // the last slab: columns behind N are zero
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int k = 0; k < AV; ++k)
+                    areg[c][k] = cg_trim<E>(areg[c][k], s * CS_K + (tid & 15) * 8 + k * (16 / (int)sizeof(E)), N);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) xreg[c] = cg_trim_codes(xreg[c], s * CS_K + (tid & 7) * 16, N);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            unsigned char *dst = smem + ((tid >> 4) + 16 * c) * (CS_A_ROW * 2) + (tid & 15) * 16;
+            if constexpr (PARTS == 1) {
+                *reinterpret_cast<uint4 *>(dst) = areg[c][0];
+            } else {
+                uint4 parts[3];
+                cg_split(areg[c], parts);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4 *>(dst + k * S::a_bytes) = parts[k];
             }
         }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int row = (tid >> 3) + 32 * c;
+            *reinterpret_cast<uint4 *>(smem + S::x_off + row * CS_X_ROW + (tid & 7) * 16) = xreg[c];
+            if ((tid & 1) == 0) *reinterpret_cast<uint32_t *>(smem + S::s_off + row * 16 + ((tid >> 1) & 3) * 4) = sreg[c] << 23;
+        }
+        if (s + 1 < nslabs) load(s + 1);
+        __syncthreads();
+        if (s * CS_K + wave * 32 >= N) continue; // nothing in this quarter
+        const unsigned char *as = smem + l32 * (CS_A_ROW * 2) + wave * 64 + 16 * lg;
+        const unsigned char *xs = smem + S::x_off + l32 * CS_X_ROW + wave * 32 + 8 * lg;
+        float sc[2];
+#pragma unroll
+        for (int a = 0; a < 2; ++a) sc[a] = *reinterpret_cast<const float *>(smem + S::s_off + (l32 + 32 * a) * 16 + wave * 4);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            uint4 xf[2], yf[2];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) xf[a] = cg_widen(Op{}, *reinterpret_cast<const uint2 *>(xs + a * 32 * CS_X_ROW + kk * 16), sc[a]);
+#pragma unroll
+            for (int part = PARTS - 1; part >= 0; --part) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+                    yf[b] = *reinterpret_cast<const uint4 *>(as + part * S::a_bytes + b * 32 * (CS_A_ROW * 2) + kk * 32);
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) acc[a][b] = mfma_32x32x16(Op{}, xf[a], yf[b], acc[a][b]);
+            }
+        }
+    }
+    __syncthreads(); // the last slab has been read: the sums take its place
+    float *sums = (float *)smem + wave * (CS_B * CS_P_ROW);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4)
+                *reinterpret_cast<float4 *>(sums + (b * 32 + l32) * CS_P_ROW + a * 32 + 8 * v4 + 4 * lg) =
+                    make_float4(acc[a][b][4 * v4], acc[a][b][4 * v4 + 1], acc[a][b][4 * v4 + 2], acc[a][b][4 * v4 + 3]);
+    uint32_t *mask = (uint32_t *)(smem + S::w_off) + 128;
+    if (wave == 0) {
+        cg_mask_end(q, (uint32_t *)(smem + S::w_off), lined_up, lane);
+        *reinterpret_cast<u32x2 *>(mask + lane * 2) = u32x2{q.words[0], q.words[1]};
+    }
+    __syncthreads();
+    // a lane's share: 16 columns of row tid / 4
+    const int row = tid >> 2, col = (tid & 3) * 16;
+    const uint32_t bits = mask[row * 2 + (col >> 5)] >> (col & 31);
+    const int64_t i = i0 + row, left = g.n - j0 - col;
+    if (i >= g.m || left <= 0) return;
+    E o[16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float4 y = *reinterpret_cast<const float4 *>((const float *)smem + row * CS_P_ROW + col + 4 * k);
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            const float4 z = *reinterpret_cast<const float4 *>((const float *)smem + (w * CS_B + row) * CS_P_ROW + col + 4 * k);
+            y.x += z.x;
+            y.y += z.y;
+            y.z += z.z;
+            y.w += z.w;
+        }
+        const float e4[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float v = ((bits >> (4 * k + e)) & 1u) ? e4[e] : 0.f; // pruned: exactly zero
+            if constexpr (PARTS == 1) o[4 * k + e] = cg_narrow(Op{}, v);
+            else o[4 * k + e] = v;
+        }
+    }
+    E *dst = DW + i * lddw + j0 + col;
+    if (left >= 16) {
+        struct __attribute__((packed, aligned(sizeof(E)))) Piece { // at any element's address
+            uint32_t x, y, z, w;
+        };
+        uint4 v[sizeof(o) / 16];
+        __builtin_memcpy(v, o, sizeof(o));
+#pragma unroll
+        for (int k = 0; k < (int)(sizeof(o) / 16); ++k) reinterpret_cast<Piece *>(dst)[k] = {v[k].x, v[k].y, v[k].z, v[k].w};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e < left) dst[e] = o[e];
     }
 }
 
@@ -331,13 +545,20 @@ static int launch_t(const Geom &g, const void *dDY, int64_t lddy, const void *dC
 {
     typedef typename CgTypes<Tag>::elem E;
     const int64_t iblocks = (g.m + CG_B - 1) / CG_B, jblocks = (g.n + CG_B - 1) / CG_B, blocks = iblocks * jblocks;
-    const int64_t at_once = CgTypes<Tag>::waves * (int64_t)compute_units_of(stream);
+    const int64_t cus = compute_units_of(stream), at_once = CgTypes<Tag>::waves * cus;
+    if (2 * blocks <= cus) { // then all of the small ones run at once, two a compute unit
+        const int64_t ji = (g.n + CS_B - 1) / CS_B, small = (g.m + CS_B - 1) / CS_B * ji;
+        auto kern = checkpoint_grad_small_kernel<Tag>;
+        LRBI_SET_MAX_LDS(kern, SmemCs<Tag>::bytes);
+        LRBI_LAUNCH(kern, dim3((unsigned)small), dim3(CG_THREADS), SmemCs<Tag>::bytes, stream, g, (const E *)dDY, lddy, (const unsigned char *)dCodes,
+                    ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, ji);
+        return LRBI_OK;
+    }
     const int64_t groups = blocks < at_once ? blocks : at_once;
-    const int w_vec_ok = ((uintptr_t)dDW & 15) == 0 && lddw * (int64_t)sizeof(E) % 16 == 0;
     auto kern = checkpoint_grad_kernel<Tag>;
     LRBI_SET_MAX_LDS(kern, SmemCg<Tag>::bytes);
     LRBI_LAUNCH(kern, dim3((unsigned)groups), dim3(CG_THREADS), SmemCg<Tag>::bytes, stream, g, (const E *)dDY, lddy, (const unsigned char *)dCodes,
-                ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, jblocks, blocks, w_vec_ok);
+                ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, jblocks, blocks);
     return LRBI_OK;
 }
 

@@ -167,6 +167,38 @@ def test_nan_codes_reach_their_weights():
                                                ("f16", 2304, 4096, 256, 256, 16, 1024), ("bf16", 4096, 9216, 256, 256, 16, 96)])
 def test_grad_of_large_layers(dtype, m, n, r, c, k, N):
     print("checkpoint grad, large", dtype, m, n, r, c, k, N, flush=True)
+    _large(dtype, m, n, r, c, k, N)
+
+
+# more 128 x 128 blocks than half the compute units, and more than are resident at once; rows that no alignment holds for
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n,r,c,k,N", [(1500, 1603, 100, 100, 12, 77), (2000, 1500, 128, 64, 40, 130), (1666, 2500, 250, 300, 70, 3),
+                                         (64, 20001, 64, 64, 64, 200), (4000, 4001, 250, 250, 16, 65)])
+def test_grad_of_many_blocks(dtype, m, n, r, c, k, N):
+    print("checkpoint grad, many blocks", dtype, m, n, r, c, k, N, flush=True)
+    _large(dtype, m, n, r, c, k, N)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n", [(100, 130), (1700, 1500)])
+def test_codes_behind_the_batch_do_not_count(dtype, m, n):
+    """The first 70 of a checkpoint's 128 columns; what stands behind them in their last block, NaN too, is left alone."""
+    print("checkpoint grad, columns behind", dtype, m, n, flush=True)
+    d = lrbi.Desc(m, n, 100, 128, 8)
+    ip, iz = device_factors(d, *workloads.make_factors(np.random.default_rng(3), d.tiles, 100, 128, 8, 0.3))
+    gen = torch.Generator(device=dev()).manual_seed(m)
+    X = torch.randn(n, 128, device=dev(), generator=gen).to(TORCH_DTYPE[dtype])
+    dY = torch.randn(m, 70, device=dev(), generator=gen).to(TORCH_DTYPE[dtype])
+    codes, scales = lrbi.checkpoint_pack(X)
+    cut = codes.clone()
+    cut[:, 70:] = 0
+    want = lrbi.checkpoint_grad(d, dY, cut[:, :96], scales[:, :3], ip, iz)
+    codes[:, 70:72] = 0x7F
+    codes[::3, 79:96] = 0xFF
+    assert torch.isfinite(want).all() and torch.equal(lrbi.checkpoint_grad(d, dY, codes[:, :96], scales[:, :3], ip, iz), want)
+
+
+def _large(dtype, m, n, r, c, k, N):
     rng = np.random.default_rng(N)
     d = lrbi.Desc(m, n, r, c, k)
     ip, iz = device_factors(d, *workloads.make_factors(rng, d.tiles, r, c, k, 0.15))
