@@ -194,14 +194,16 @@ def unpack_mask(desc: Desc, mask_bytes: np.ndarray) -> np.ndarray:
 # stream's handle comes without an object around it.
 _codes = None
 _current_stream = None
+_current_device = None
 _f32 = _i64 = None
 
 
 def _look_up_torch():
-    global _codes, _current_stream, _f32, _i64
+    global _codes, _current_stream, _current_device, _f32, _i64
     import torch
     _f32, _i64 = torch.float32, torch.int64
     raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    _current_device = device or torch.cuda.current_device
     if raw and device:
         _current_stream = lambda: raw(device())  # noqa: E731
     else:
@@ -220,6 +222,17 @@ def _stream_ptr(stream):
 def _dev_ptr(t, what):
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % what)
+    return t.data_ptr()
+
+
+def _here_ptr(t, what):
+    """As _dev_ptr, of a tensor of the device that the call runs on."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % what)
+    if _current_device is None:
+        _look_up_torch()
+    if t.get_device() != _current_device():
+        raise ValueError("%s is not on the current device" % what)
     return t.data_ptr()
 
 
@@ -578,7 +591,7 @@ def _store(pair, rows, cols, block_bytes):
         raise ValueError("codes and scales must be row-major")
     if rows == 1:  # a single row may have any stride: its pitch is what it holds
         ldc, lds = ccols // 16 * 16, scols // 4 * 4
-    return _dev_ptr(codes, "codes"), ldc, _dev_ptr(scales, "scales"), lds
+    return _here_ptr(codes, "codes"), ldc, _here_ptr(scales, "scales"), lds
 
 
 def _new_store(rows, cols, block_bytes, device):
@@ -599,8 +612,8 @@ def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
         out = _new_store(desc.m, desc.n, 16, W.device)
     cp, ldc, sp, lds = _store(out, desc.m, desc.n, 16)
     _check(load_library().lrbi_quant_pack(
-        ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), W.stride(0), None if dIp is None else _dev_ptr(dIp, "Ip"),
-        None if dIz is None else _dev_ptr(dIz, "Iz"), cp, ldc, sp, lds, _stream_ptr(stream)), "lrbi_quant_pack")
+        ctypes.byref(desc), _dtype_code(W), _here_ptr(W, "W"), W.stride(0), None if dIp is None else _here_ptr(dIp, "Ip"),
+        None if dIz is None else _here_ptr(dIz, "Iz"), cp, ldc, sp, lds, _stream_ptr(stream)), "lrbi_quant_pack")
     return out
 
 
@@ -618,7 +631,7 @@ def quant_unpack(codes, scales, n: int, dtype, out=None, stream=None):
     m = codes.shape[0]
     out = _values_out(out, m, n, dtype, codes.device)
     cp, ldc, sp, lds = _store((codes, scales), m, n, 16)
-    _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _dev_ptr(out, "W"), out.stride(0),
+    _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _here_ptr(out, "W"), out.stride(0),
                                             _stream_ptr(stream)), "lrbi_quant_unpack")
     return out
 
@@ -636,7 +649,7 @@ def quant_matvec(codes, scales, X, out=None, stream=None):
     if squeeze and out is not None:
         out = out.unsqueeze(1)
     out, ldy = _row_major_out(out, m, N, X)
-    _check(load_library().lrbi_quant_matvec(_dtype_code(X), cp, ldc, sp, lds, m, n, _dev_ptr(X, "X"), ldx, N, _dev_ptr(out, "Y"), ldy,
+    _check(load_library().lrbi_quant_matvec(_dtype_code(X), cp, ldc, sp, lds, m, n, _here_ptr(X, "X"), ldx, N, _here_ptr(out, "Y"), ldy,
                                             _stream_ptr(stream)), "lrbi_quant_matvec")
     return out[:, 0] if squeeze else out
 
@@ -650,7 +663,7 @@ def checkpoint_pack(X, out=None, stream=None):
     if out is None:
         out = _new_store(n, N, 32, X.device)
     cp, ldc, sp, lds = _store(out, n, N, 32)
-    _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), _dev_ptr(X, "X"), X.stride(0), n, N, cp, ldc, sp, lds,
+    _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), _here_ptr(X, "X"), X.stride(0), n, N, cp, ldc, sp, lds,
                                                _stream_ptr(stream)), "lrbi_checkpoint_pack")
     return out
 
@@ -660,7 +673,7 @@ def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
     n = codes.shape[0]
     out = _values_out(out, n, N, dtype, codes.device)
     cp, ldc, sp, lds = _store((codes, scales), n, N, 32)
-    _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _dev_ptr(out, "X"), out.stride(0),
+    _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _here_ptr(out, "X"), out.stride(0),
                                                  _stream_ptr(stream)), "lrbi_checkpoint_unpack")
     return out
 
@@ -676,8 +689,8 @@ def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=No
     cp, ldc, sp, lds = _store((codes, scales), n, N, 32)
     out, lddw = _row_major_out(out, m, n, dY)
     _check(load_library().lrbi_checkpoint_grad(
-        ctypes.byref(desc), _dtype_code(dY), _dev_ptr(dY, "dY"), dY.stride(0), cp, ldc, sp, lds, N, _dev_ptr(dIp, "Ip"),
-        _dev_ptr(dIz, "Iz"), _dev_ptr(out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
+        ctypes.byref(desc), _dtype_code(dY), _here_ptr(dY, "dY"), dY.stride(0), cp, ldc, sp, lds, N, _here_ptr(dIp, "Ip"),
+        _here_ptr(dIz, "Iz"), _here_ptr(out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
     return out
 
 
@@ -697,7 +710,7 @@ def token_logprobs_workspace_bytes(dtype_code: int, V: int, N: int, top: int = 0
 def _row_ptr(t, dtype, shape, what):
     if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s" % (what, dtype, tuple(shape)))
-    return _dev_ptr(t, what)
+    return _here_ptr(t, what)
 
 
 def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, stream=None):
@@ -723,15 +736,16 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, 
         raise ValueError("out is of a call with other results")
     if workspace is None:
         import torch
-        workspace = torch.empty(token_logprobs_workspace_bytes(code, V, N, top), dtype=torch.uint8, device=logits.device)
+        with torch.cuda.stream(stream):  # it belongs to the stream that uses it
+            workspace = torch.empty(token_logprobs_workspace_bytes(code, V, N, top), dtype=torch.uint8, device=logits.device)
     row, tok_ptr, logp_ptr, ids_ptr, top_ptr = (N,), None, None, None, None
     if tokens is not None:
         tok_ptr, logp_ptr = _row_ptr(tokens, _i64, row, "tokens"), _row_ptr(logp, _f32, row, "out.logp")
     if top > 0:
         ids_ptr, top_ptr = _row_ptr(top_ids, _i64, (top, N), "out.top_ids"), _row_ptr(top_logp, _f32, (top, N), "out.top_logp")
-    ws_ptr, ws_bytes = _scratch(workspace)
+    ws_ptr, ws_bytes = _here_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
     _check(load_library().lrbi_token_logprobs(
-        code, _dev_ptr(logits, "logits"), ldl, V, N, tok_ptr, logp_ptr, _row_ptr(entropy, _f32, row, "out.entropy"),
+        code, _here_ptr(logits, "logits"), ldl, V, N, tok_ptr, logp_ptr, _row_ptr(entropy, _f32, row, "out.entropy"),
         _row_ptr(stats, _f32, (2, N), "out.stats"), top, ids_ptr, top_ptr, ws_ptr, ws_bytes, _stream_ptr(stream)), "lrbi_token_logprobs")
     return out
 
@@ -750,8 +764,8 @@ def token_logprobs_grad(logits, tokens, result, g_logp=None, g_entropy=None, out
     out, lddl = _row_major_out(out, V, N, logits)
     row = (N,)
     _check(load_library().lrbi_token_logprobs_grad(
-        code, _dev_ptr(logits, "logits"), ldl, V, N, None if tokens is None else _row_ptr(tokens, _i64, row, "tokens"),
+        code, _here_ptr(logits, "logits"), ldl, V, N, None if tokens is None else _row_ptr(tokens, _i64, row, "tokens"),
         _row_ptr(result.stats, _f32, (2, N), "stats"), _row_ptr(result.entropy, _f32, row, "entropy"),
         None if g_logp is None else _row_ptr(g_logp, _f32, row, "g_logp"), None if g_entropy is None else _row_ptr(g_entropy, _f32, row, "g_entropy"),
-        _dev_ptr(out, "out"), lddl, _stream_ptr(stream)), "lrbi_token_logprobs_grad")
+        _here_ptr(out, "out"), lddl, _stream_ptr(stream)), "lrbi_token_logprobs_grad")
     return out

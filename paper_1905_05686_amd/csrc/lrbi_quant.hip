@@ -341,6 +341,7 @@ static int launch_matvec_t(const unsigned char *codes, int64_t ldc, const unsign
     // 12); one 16-bit column is little to share (300 x 16384 9.7 / 14 / 22, 16384 x 16384 34.8 / 38.6 / 34.5).
     int wr = m >= 64 * 256 ? 4 : m >= 32 * 256 || cols * PARTS > 8 ? 2 : 1;
     if (column && sizeof(T) == 2) wr = 1;
+    if (cols * PARTS > 31) wr = 4; // X of a round of two rows' wavefronts and the sums are 162 KB
     const int64_t row_blocks = (m + 16 * wr - 1) / (16 * wr), col_blocks = (N + cols - 1) / cols;
     // X of a chunk in LDS: all of it where it fits, otherwise whole rounds of the wavefronts
     const int64_t round = (int64_t)QM_QUAD * (QM_WAVES / wr), per_row = (int64_t)cols * PARTS * 2, all = (n + QM_QUAD - 1) / QM_QUAD * QM_QUAD;
