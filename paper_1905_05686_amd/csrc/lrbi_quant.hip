@@ -150,7 +150,7 @@ __device__ __forceinline__ void qm_load(QmQuad &w, const unsigned char *crow, co
 }
 
 // NT: tiles of 16 operand columns.  cols: columns of X that a workgroup takes at a time; chunk: columns of W whose X is in LDS at a
-// time, a multiple of 512 (8 / WR).  VX: columns of X that are loaded together (they divide cols and N and are aligned); 0: a
+// time, a multiple of 512 (8 / WR).  VX: columns of X that are loaded together (at any element's address; cols is at least VX); 0: a
 // single column, contiguous and 16-byte aligned.
 template <typename T, int NT, int WR, int VX>
 __global__ __launch_bounds__(64 * QM_WAVES) void quant_matvec_kernel(const unsigned char *__restrict__ codes, int64_t ldc,
@@ -166,10 +166,9 @@ __global__ __launch_bounds__(64 * QM_WAVES) void quant_matvec_kernel(const unsig
     const int64_t blk = wide_block();
     const int64_t cb = blk / workgroups;
     int64_t rb = blk - cb * workgroups;
-    const int64_t q0 = cb * cols;
-    if (q0 >= N) return;
-    const int nc = N - q0 < cols ? (int)(N - q0) : cols; // columns of X here
-    const int ops = nc * PARTS;                          // operand columns
+    if (cb * cols >= N) return;
+    const int64_t q0 = cb * cols < N - cols ? cb * cols : N - cols; // (the last ones may be the neighbour's too: the same sums)
+    const int ops = cols * PARTS;                        // operand columns
     uint4 *Xs = lrbi_dyn_smem;                           // [chunk / 8][ops]
     float *red = (float *)(Xs + chunk / 8 * ops);        // [two in turn][wave][tile][16 rows][16 columns + 1]
     const int r = lane & 15, blkq = lane >> 4;
@@ -203,13 +202,13 @@ __global__ __launch_bounds__(64 * QM_WAVES) void quant_matvec_kernel(const unsig
     for (int64_t k0 = 0; k0 < n; k0 += chunk) {
         const int kk = (int)(k0 + chunk < quads * QM_QUAD ? chunk : quads * QM_QUAD - k0); // a multiple of 512
         constexpr int V = VX ? VX : 1; // eight rows of V columns a lane
-        const int per_row = nc / V;
+        const int per_row = (cols + V - 1) / V;
         const bool fill = !once || rb == blk - cb * workgroups;
         if (!once) __syncthreads(); // the last chunk has been read
         for (int e = fill ? tid : kk; e < kk / 8 * per_row; e += 64 * QM_WAVES) {
-            const int j8 = e / per_row, c = (e - j8 * per_row) * V;
+            const int j8 = e / per_row, c4 = (e - j8 * per_row) * V, c = c4 < cols - V ? c4 : cols - V; // (the last V)
             const int64_t j = k0 + 8 * j8;
-            struct alignas(V * sizeof(T)) Row {
+            struct __attribute__((packed, aligned(sizeof(T)))) Row {
                 T v[V];
             } x[8];
             if (VX == 0 && j + 8 <= n) {
@@ -268,8 +267,8 @@ __global__ __launch_bounds__(64 * QM_WAVES) void quant_matvec_kernel(const unsig
 #pragma unroll
         for (int v = 0; v < 4; ++v) part[((wave * NT + t) * 16 + 4 * blkq + v) * 17 + r] = acc[t][v];
     __syncthreads();
-    for (int e = tid; e < 16 * WR * nc; e += 64 * QM_WAVES) {
-        const int il = e / nc, c = e - il * nc;
+    for (int e = tid; e < 16 * WR * cols; e += 64 * QM_WAVES) {
+        const int il = e / cols, c = e - il * cols;
         float y = 0.f;
 #pragma unroll
         for (int p = PARTS - 1; p >= 0; --p) { // the small parts first
@@ -331,27 +330,29 @@ static int launch_matvec_t(const unsigned char *codes, int64_t ldc, const unsign
 {
     constexpr int PARTS = QmOperand<T>::parts;
     const int nt = N * PARTS <= 16 ? 1 : 2;
-    const int most = 16 * nt / PARTS, cols = N < most ? (int)N : most;
-    const int64_t bits = (int64_t)(uintptr_t)X | ldx * (int64_t)sizeof(T);
+    const int most = 16 * nt / PARTS;
+    const int64_t col_blocks = (N + most - 1) / most;
+    const int cols = (int)((N + col_blocks - 1) / col_blocks);
     const bool column = N == 1 && ldx == 1 && ((uintptr_t)X & 15) == 0;
-    const bool fours = N % 4 == 0 && cols % 4 == 0 && (bits & (4 * sizeof(T) - 1)) == 0;
+    const bool fours = cols >= 4;
     // Wavefronts on different rows share X in LDS and add up fewer sums; there are fewer workgroups.  As many as leave one for
     // every compute unit (us, with 1, 2, 4: 8192 x 8192, 7 columns f16 28 / 22 / 25; 16384 x 4096, 8 columns 20 / 14.5 / 12;
     // 2000 x 4000, 3 columns 8.6 / 8.5 / 10), two for more than 8 operand columns, whose X fills LDS (6000 x 3000, 20 columns 13 / 10 /
     // 12); one 16-bit column is little to share (300 x 16384 9.7 / 14 / 22, 16384 x 16384 34.8 / 38.6 / 34.5).
     int wr = m >= 64 * 256 ? 4 : m >= 32 * 256 || cols * PARTS > 8 ? 2 : 1;
     if (column && sizeof(T) == 2) wr = 1;
-    if (cols * PARTS > 31) wr = 4; // X of a round of two rows' wavefronts and the sums are 162 KB
-    const int64_t row_blocks = (m + 16 * wr - 1) / (16 * wr), col_blocks = (N + cols - 1) / cols;
+    const int64_t row_blocks = (m + 16 * wr - 1) / (16 * wr);
     // X of a chunk in LDS: all of it where it fits, otherwise whole rounds of the wavefronts
     const int64_t round = (int64_t)QM_QUAD * (QM_WAVES / wr), per_row = (int64_t)cols * PARTS * 2, all = (n + QM_QUAD - 1) / QM_QUAD * QM_QUAD;
     int64_t chunk = QM_LDS / per_row / round * round;
     if (chunk < round) chunk = round;
     if (chunk > all) chunk = all;
-    // workgroups that keep X take several blocks of rows: two on a compute unit
-    const int64_t workgroups = chunk == all && row_blocks > 512 ? 512 : row_blocks, groups = workgroups * col_blocks;
+    // workgroups that keep X take several blocks of rows, with two sets of sums: two on a compute unit
+    const int64_t x_bytes = chunk * per_row, sums = (int64_t)QM_WAVES * nt * 16 * 17 * 4;
+    const bool several = chunk == all && row_blocks > 512 && x_bytes + 2 * sums <= 160 * 1024;
+    const int64_t workgroups = several ? 512 : row_blocks, groups = workgroups * col_blocks;
     if (groups > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    const size_t smem = (size_t)(chunk * per_row) + (size_t)2 * QM_WAVES * nt * 16 * 17 * 4;
+    const size_t smem = (size_t)(x_bytes + (several ? 2 : 1) * sums); // at most 145 KB
 #define LRBI_QM(NT, WR) (fours ? quant_matvec_kernel<T, NT, WR, 4> : quant_matvec_kernel<T, NT, WR, 1>)
     auto kern = nt == 2   ? (wr == 4 ? LRBI_QM(2, 4) : LRBI_QM(2, 2))
                 : !column ? (wr == 4 ? LRBI_QM(1, 4) : wr == 2 ? LRBI_QM(1, 2) : LRBI_QM(1, 1))

@@ -115,7 +115,7 @@ def test_strided_buffers_and_untouched_bytes():
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("m,n,N", [(1, 1, 1), (1, 33, 1), (16, 32, 1), (17, 100, 1), (500, 800, 1), (300, 2048, 1), (33, 2049, 1), (100, 6000, 1),
                                    (31, 70, 2), (64, 512, 5), (50, 300, 6), (40, 2100, 10), (65, 257, 16), (20, 96, 17), (48, 4200, 20),
-                                   (30, 130, 33), (16, 64, 70), (40, 4100, 31), (40, 4100, 32), (33, 2600, 67), (2000, 1500, 1), (70, 20000, 3)])
+                                   (30, 130, 33), (16, 64, 70), (40, 4100, 31), (40, 4100, 32), (33, 2600, 67), (50, 2000, 35), (20000, 70, 33), (2000, 1500, 1), (70, 20000, 3)])
 def test_matvec(dtype, m, n, N):
     print("quant matvec", dtype, m, n, N, flush=True)
     rng = np.random.default_rng(m + n + N)
