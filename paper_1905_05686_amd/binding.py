@@ -225,14 +225,21 @@ def _dev_ptr(t, what):
     return t.data_ptr()
 
 
-def _here_ptr(t, what):
-    """As _dev_ptr, of a tensor of the device that the call runs on."""
-    if not t.is_cuda:
+def _device_of(t, what):
+    """The device of a call, that of its first tensor: the current one."""
+    device = t.get_device()
+    if device < 0:
         raise ValueError("%s must be a device tensor" % what)
     if _current_device is None:
         _look_up_torch()
-    if t.get_device() != _current_device():
+    if device != _current_device():
         raise ValueError("%s is not on the current device" % what)
+    return device
+
+
+def _ptr_on(device, t, what):
+    if t.get_device() != device:
+        raise ValueError("%s must be a device tensor, on the same device as the others" % what)
     return t.data_ptr()
 
 
@@ -575,7 +582,7 @@ def nmf(desc: Desc, W, Mp, Mz, iters: int, eps: float = 1e-9, method: int = 1, w
     return Mp, Mz
 
 
-def _store(pair, rows, cols, block_bytes):
+def _store(device, pair, rows, cols, block_bytes):
     """Addresses and pitches of codes and scales that hold `rows` rows of `cols` values in blocks of 32."""
     codes, scales = pair
     blocks = -(-cols // 32)
@@ -591,7 +598,7 @@ def _store(pair, rows, cols, block_bytes):
         raise ValueError("codes and scales must be row-major")
     if rows == 1:  # a single row may have any stride: its pitch is what it holds
         ldc, lds = ccols // 16 * 16, scols // 4 * 4
-    return _here_ptr(codes, "codes"), ldc, _here_ptr(scales, "scales"), lds
+    return _ptr_on(device, codes, "codes"), ldc, _ptr_on(device, scales, "scales"), lds
 
 
 def _new_store(rows, cols, block_bytes, device):
@@ -608,12 +615,13 @@ def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
     reuses two tensors.  Returns (codes, scales)."""
     if W.dim() != 2 or W.shape != (desc.m, desc.n) or (desc.n > 1 and W.stride(1) != 1):
         raise ValueError("W must be a row-major [m, n] tensor")
+    device = _device_of(W, "W")
     if out is None:
         out = _new_store(desc.m, desc.n, 16, W.device)
-    cp, ldc, sp, lds = _store(out, desc.m, desc.n, 16)
+    cp, ldc, sp, lds = _store(device, out, desc.m, desc.n, 16)
     _check(load_library().lrbi_quant_pack(
-        ctypes.byref(desc), _dtype_code(W), _here_ptr(W, "W"), W.stride(0), None if dIp is None else _here_ptr(dIp, "Ip"),
-        None if dIz is None else _here_ptr(dIz, "Iz"), cp, ldc, sp, lds, _stream_ptr(stream)), "lrbi_quant_pack")
+        ctypes.byref(desc), _dtype_code(W), W.data_ptr(), W.stride(0), None if dIp is None else _ptr_on(device, dIp, "Ip"),
+        None if dIz is None else _ptr_on(device, dIz, "Iz"), cp, ldc, sp, lds, _stream_ptr(stream)), "lrbi_quant_pack")
     return out
 
 
@@ -629,9 +637,10 @@ def _values_out(out, rows, cols, dtype, device):
 def quant_unpack(codes, scales, n: int, dtype, out=None, stream=None):
     """lrbi_quant_unpack: the values [m, n] of 4-bit codes, as numbers of `dtype`."""
     m = codes.shape[0]
+    device = _device_of(codes, "codes")
     out = _values_out(out, m, n, dtype, codes.device)
-    cp, ldc, sp, lds = _store((codes, scales), m, n, 16)
-    _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _here_ptr(out, "W"), out.stride(0),
+    cp, ldc, sp, lds = _store(device, (codes, scales), m, n, 16)
+    _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _ptr_on(device, out, "W"), out.stride(0),
                                             _stream_ptr(stream)), "lrbi_quant_unpack")
     return out
 
@@ -645,11 +654,12 @@ def quant_matvec(codes, scales, X, out=None, stream=None):
     ldx, x1 = X.stride()
     if N > 1 and x1 != 1:
         raise ValueError("X must be a row-major tensor")
-    cp, ldc, sp, lds = _store((codes, scales), m, n, 16)
+    device = _device_of(X, "X")
+    cp, ldc, sp, lds = _store(device, (codes, scales), m, n, 16)
     if squeeze and out is not None:
         out = out.unsqueeze(1)
     out, ldy = _row_major_out(out, m, N, X)
-    _check(load_library().lrbi_quant_matvec(_dtype_code(X), cp, ldc, sp, lds, m, n, _here_ptr(X, "X"), ldx, N, _here_ptr(out, "Y"), ldy,
+    _check(load_library().lrbi_quant_matvec(_dtype_code(X), cp, ldc, sp, lds, m, n, X.data_ptr(), ldx, N, _ptr_on(device, out, "Y"), ldy,
                                             _stream_ptr(stream)), "lrbi_quant_matvec")
     return out[:, 0] if squeeze else out
 
@@ -660,10 +670,11 @@ def checkpoint_pack(X, out=None, stream=None):
     if X.dim() != 2 or (X.shape[1] > 1 and X.stride(1) != 1):
         raise ValueError("X must be a row-major [n, N] tensor")
     n, N = X.shape
+    device = _device_of(X, "X")
     if out is None:
         out = _new_store(n, N, 32, X.device)
-    cp, ldc, sp, lds = _store(out, n, N, 32)
-    _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), _here_ptr(X, "X"), X.stride(0), n, N, cp, ldc, sp, lds,
+    cp, ldc, sp, lds = _store(device, out, n, N, 32)
+    _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), X.data_ptr(), X.stride(0), n, N, cp, ldc, sp, lds,
                                                _stream_ptr(stream)), "lrbi_checkpoint_pack")
     return out
 
@@ -671,9 +682,10 @@ def checkpoint_pack(X, out=None, stream=None):
 def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
     """lrbi_checkpoint_unpack: the values [n, N] of a checkpoint, as numbers of `dtype`."""
     n = codes.shape[0]
+    device = _device_of(codes, "codes")
     out = _values_out(out, n, N, dtype, codes.device)
-    cp, ldc, sp, lds = _store((codes, scales), n, N, 32)
-    _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _here_ptr(out, "X"), out.stride(0),
+    cp, ldc, sp, lds = _store(device, (codes, scales), n, N, 32)
+    _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _ptr_on(device, out, "X"), out.stride(0),
                                                  _stream_ptr(stream)), "lrbi_checkpoint_unpack")
     return out
 
@@ -686,11 +698,12 @@ def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=No
     N = dY.shape[1]
     if N > 1 and dY.stride(1) != 1:
         raise ValueError("dY must be a row-major tensor")
-    cp, ldc, sp, lds = _store((codes, scales), n, N, 32)
+    device = _device_of(dY, "dY")
+    cp, ldc, sp, lds = _store(device, (codes, scales), n, N, 32)
     out, lddw = _row_major_out(out, m, n, dY)
     _check(load_library().lrbi_checkpoint_grad(
-        ctypes.byref(desc), _dtype_code(dY), _here_ptr(dY, "dY"), dY.stride(0), cp, ldc, sp, lds, N, _here_ptr(dIp, "Ip"),
-        _here_ptr(dIz, "Iz"), _here_ptr(out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
+        ctypes.byref(desc), _dtype_code(dY), dY.data_ptr(), dY.stride(0), cp, ldc, sp, lds, N, _ptr_on(device, dIp, "Ip"),
+        _ptr_on(device, dIz, "Iz"), _ptr_on(device, out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
     return out
 
 
@@ -707,10 +720,10 @@ def token_logprobs_workspace_bytes(dtype_code: int, V: int, N: int, top: int = 0
     return out.value
 
 
-def _row_ptr(t, dtype, shape, what):
+def _row_ptr(device, t, dtype, shape, what):
     if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s" % (what, dtype, tuple(shape)))
-    return _here_ptr(t, what)
+    return _ptr_on(device, t, what)
 
 
 def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, stream=None):
@@ -723,7 +736,7 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, 
     ldl, inner = logits.stride()
     if N > 1 and inner != 1:
         raise ValueError("logits must be a row-major [V, N] tensor")
-    code = _dtype_code(logits)
+    code, device = _dtype_code(logits), _device_of(logits, "logits")
     if out is None:
         if top < 0:
             raise ValueError("top must not be negative")
@@ -740,13 +753,13 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, 
             workspace = torch.empty(token_logprobs_workspace_bytes(code, V, N, top), dtype=torch.uint8, device=logits.device)
     row, tok_ptr, logp_ptr, ids_ptr, top_ptr = (N,), None, None, None, None
     if tokens is not None:
-        tok_ptr, logp_ptr = _row_ptr(tokens, _i64, row, "tokens"), _row_ptr(logp, _f32, row, "out.logp")
+        tok_ptr, logp_ptr = _row_ptr(device, tokens, _i64, row, "tokens"), _row_ptr(device, logp, _f32, row, "out.logp")
     if top > 0:
-        ids_ptr, top_ptr = _row_ptr(top_ids, _i64, (top, N), "out.top_ids"), _row_ptr(top_logp, _f32, (top, N), "out.top_logp")
-    ws_ptr, ws_bytes = _here_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+        ids_ptr, top_ptr = _row_ptr(device, top_ids, _i64, (top, N), "out.top_ids"), _row_ptr(device, top_logp, _f32, (top, N), "out.top_logp")
+    ws_ptr, ws_bytes = _ptr_on(device, workspace, "workspace"), workspace.numel() * workspace.element_size()
     _check(load_library().lrbi_token_logprobs(
-        code, _here_ptr(logits, "logits"), ldl, V, N, tok_ptr, logp_ptr, _row_ptr(entropy, _f32, row, "out.entropy"),
-        _row_ptr(stats, _f32, (2, N), "out.stats"), top, ids_ptr, top_ptr, ws_ptr, ws_bytes, _stream_ptr(stream)), "lrbi_token_logprobs")
+        code, logits.data_ptr(), ldl, V, N, tok_ptr, logp_ptr, _row_ptr(device, entropy, _f32, row, "out.entropy"),
+        _row_ptr(device, stats, _f32, (2, N), "out.stats"), top, ids_ptr, top_ptr, ws_ptr, ws_bytes, _stream_ptr(stream)), "lrbi_token_logprobs")
     return out
 
 
@@ -760,12 +773,12 @@ def token_logprobs_grad(logits, tokens, result, g_logp=None, g_entropy=None, out
     ldl, inner = logits.stride()
     if N > 1 and inner != 1:
         raise ValueError("logits must be a row-major [V, N] tensor")
-    code = _dtype_code(logits)
+    code, device = _dtype_code(logits), _device_of(logits, "logits")
     out, lddl = _row_major_out(out, V, N, logits)
     row = (N,)
     _check(load_library().lrbi_token_logprobs_grad(
-        code, _here_ptr(logits, "logits"), ldl, V, N, None if tokens is None else _row_ptr(tokens, _i64, row, "tokens"),
-        _row_ptr(result.stats, _f32, (2, N), "stats"), _row_ptr(result.entropy, _f32, row, "entropy"),
-        None if g_logp is None else _row_ptr(g_logp, _f32, row, "g_logp"), None if g_entropy is None else _row_ptr(g_entropy, _f32, row, "g_entropy"),
-        _here_ptr(out, "out"), lddl, _stream_ptr(stream)), "lrbi_token_logprobs_grad")
+        code, logits.data_ptr(), ldl, V, N, None if tokens is None else _row_ptr(device, tokens, _i64, row, "tokens"),
+        _row_ptr(device, result.stats, _f32, (2, N), "stats"), _row_ptr(device, result.entropy, _f32, row, "entropy"),
+        None if g_logp is None else _row_ptr(device, g_logp, _f32, row, "g_logp"), None if g_entropy is None else _row_ptr(device, g_entropy, _f32, row, "g_entropy"),
+        _ptr_on(device, out, "out"), lddl, _stream_ptr(stream)), "lrbi_token_logprobs_grad")
     return out
