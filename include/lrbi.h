@@ -518,7 +518,7 @@ int lrbi_checkpoint_grad(const lrbi_desc *desc, lrbi_dtype dtype, const void *dD
  *   logit -infinity, no top words.  A column that holds a NaN or +infinity: NaN log p and entropy (top words: by their logits).
  *   dWorkspace: required, 16-byte aligned, at least lrbi_token_logprobs_workspace_bytes bytes (LRBI_ERR_WORKSPACE
  *   otherwise).  fp32 arithmetic in a fixed order (identical bits from call to call).  Two kernel launches, one for
- *   a single contiguous 16-byte aligned column (N = ldl = 1) of up to 32768 words.
+ *   a single contiguous column (N = ldl = 1) of up to 32768 words.
  *
  * lrbi_token_logprobs_grad: the gradient of sum_q (dGLogp[q] dLogp[q] + dGEntropy[q] dEntropy[q]) with respect to the logits:
  *   dDL[v][q] = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy), V x N of `dtype`, lddl >= N.  It is the dY of

@@ -54,10 +54,20 @@ template <> struct Logit<__hip_bfloat16> {
     __device__ static __hip_bfloat16 narrow(float v) { return __builtin_bit_cast(__hip_bfloat16, (__bf16)v); } // nearest-even
 };
 
-// P values of a row as one load or store
-template <typename T, int P> struct alignas(sizeof(T) * P) Piece {
+// P values of a row as one load or store, at any element's address
+template <typename T, int P> struct __attribute__((packed, aligned(sizeof(T)))) Piece {
     T v[P];
 };
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Piece16 {
+    uint32_t v[4];
+};
+// first column of a lane's piece: the last piece of a row that P does not divide (WHOLE: it does) begins earlier, at columns that it
+// shares with its neighbour
+template <int P, bool WHOLE> __device__ __forceinline__ int64_t lp_first(int64_t piece, int64_t N)
+{
+    const int64_t q = piece * P;
+    return WHOLE || q + P <= N ? q : N - P;
+}
 
 __device__ __forceinline__ float lp_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
 // d as a factor of 2^d, which is 0 from -150 on: no infinity is multiplied with that 0.  (A NaN goes through 2^d.)
@@ -113,9 +123,9 @@ __device__ __forceinline__ void lp_load(Piece<T, P> (&x)[ROWS], const T *src, in
         }
     } else if constexpr (COLUMN) {
         constexpr int N16 = ROWS * sizeof(T) / 16;
-        uint4 v[N16];
+        Piece16<T> v[N16];
 #pragma unroll
-        for (int i = 0; i < N16; ++i) v[i] = reinterpret_cast<const uint4 *>(src)[i];
+        for (int i = 0; i < N16; ++i) v[i] = reinterpret_cast<const Piece16<T> *>(src)[i];
         __builtin_memcpy(x, v, sizeof(x));
     } else {
 #pragma unroll
@@ -135,7 +145,7 @@ __device__ __forceinline__ float lp_second(uint32_t more) { return __builtin_bit
 
 // One pass: lane (tx, ty) of a workgroup takes columns (block * tx_count + tx) P .. + P - 1 and the `runs` runs of 32 rows
 // from ((slice * ty_count) + ty) * runs on.  part: [column][slice]; TOP: run_max, run_more: [column][run_pitch].
-template <typename T, int P, bool COLUMN, bool TOP>
+template <typename T, int P, bool WHOLE, bool COLUMN, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N,
                                                                    int tx_count, int ty_count, int64_t col_blocks, int64_t runs, int64_t slices,
                                                                    float4 *__restrict__ part, float *__restrict__ run_max,
@@ -146,14 +156,15 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__re
     const int ty = tid / tx_count, tx = tid - ty * tx_count;
     const int64_t blk = wide_block();
     const int64_t slice = blk / col_blocks, cb = blk - slice * col_blocks; // neighbours read the same rows
-    const int64_t q0 = (cb * tx_count + tx) * P;
     if (slice >= slices) return; // a workgroup past the last one
+    const int64_t mine = cb * tx_count + tx, q0 = lp_first<P, WHOLE>(mine, N);
+    const bool has = mine * P < N;
     LpSums a[P];
     float top[P]; // of the current run, and more of it
     uint32_t more[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) a[p] = lp_empty<T>();
-    if (ty < ty_count && q0 < N) {
+    if (ty < ty_count && has) {
         const int64_t run0 = (slice * ty_count + ty) * runs;
         for (int64_t run = run0; run < run0 + runs && run * LP_RUN < V; ++run) {
             float second[P];
@@ -223,8 +234,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__re
         __syncthreads();
         for (int e = tid; e < tx_count * P * ty_count; e += blockDim.x) {
             const int col = e / ty_count, y = e - col * ty_count, from = y * tx_count + col / P;
-            const int64_t q = cb * tx_count * P + col, run = slice * ty_count + y;
-            if (q < N && run * LP_RUN < V) {
+            const int64_t its = cb * tx_count + col / P, q = lp_first<P, WHOLE>(its, N) + col % P, run = slice * ty_count + y;
+            if (its * P < N && run * LP_RUN < V) {
                 run_max[q * run_pitch + run] = join[col % P][from];
                 run_more[q * run_pitch + run] = __builtin_bit_cast(uint32_t, join[P + col % P][from]);
             }
@@ -253,7 +264,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__re
             }
         }
     }
-    if (ty == 0 && q0 < N)
+    if (ty == 0 && has)
 #pragma unroll
         for (int p = 0; p < P; ++p) part[(q0 + p) * slices + slice] = make_float4(a[p].m, a[p].s, a[p].t, 0.f);
 }
@@ -517,9 +528,9 @@ __global__ __launch_bounds__(LP_COLUMN_LANES) void logprobs_column_kernel(const 
     for (int s = 0; s < LP_COLUMN_SWEEPS; ++s) {
         const int v0 = (s * LP_COLUMN_LANES + tid) * 8;
         if (v0 + 8 <= V) {
-            uint4 p[sizeof(T) / 2];
+            Piece16<T> p[sizeof(T) / 2];
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) p[i] = reinterpret_cast<const uint4 *>(L + v0)[i];
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) p[i] = reinterpret_cast<const Piece16<T> *>(L + v0)[i];
             T e[8];
             __builtin_memcpy(e, p, sizeof(e));
 #pragma unroll
@@ -592,8 +603,9 @@ __global__ __launch_bounds__(LP_COLUMN_LANES) void logprobs_column_kernel(const 
 static_assert(LP_COLUMN_LANES == 16 * 64 && LP_COLUMN_MOST / LP_RUN <= LP_ROUND, "one partial a lane of 16, one round of runs");
 
 // dx_v = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy); a lane owns P columns and the `batches` batches of 8 rows from
-// ((block * ty_count) + ty) * batches on.  DL may be L: a batch is read whole before any of it is written.
-template <typename T, int P>
+// ((block * ty_count) + ty) * batches on.  DL may be L: a batch is read whole before any of it is
+// written, and what a lane reads of a neighbour's columns it does not use.
+template <typename T, int P, bool WHOLE>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *L, int64_t ldl, int64_t V, int64_t N,
                                                                    const int64_t *__restrict__ tok, const float *__restrict__ stats,
                                                                    const float *__restrict__ entropy, const float *__restrict__ g_logp,
@@ -605,10 +617,11 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *L, i
     const int ty = tid / tx_count, tx = tid - ty * tx_count;
     const int64_t blk = wide_block();
     const int64_t rb = blk / col_blocks, cb = blk - rb * col_blocks; // neighbours read the same rows
-    const int64_t q0 = (cb * tx_count + tx) * P, first = (rb * ty_count + ty) * batches * LP_GRAD;
+    const int64_t mine = cb * tx_count + tx, q0 = lp_first<P, WHOLE>(mine, N), first = (rb * ty_count + ty) * batches * LP_GRAD;
+    const int shared = (int)(mine * P - q0); // columns that are the neighbour's to write
     for (int e = tid; e < tx_count * P; e += blockDim.x) {
-        const int64_t q = cb * tx_count * P + e;
-        if (q >= N) break;
+        const int64_t its = cb * tx_count + e / P, q = lp_first<P, WHOLE>(its, N) + e % P;
+        if (its * P >= N) break;
         const float m = fmaxf(stats[q], Logit<T>::lowest), c = lp_factor<T>(m), r = m * c;
         float log_s = stats[N + q] + __builtin_fmaf(m, c, -r);
         const int64_t w = g_logp ? tok[q] : -1;
@@ -630,7 +643,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *L, i
         column[6][e] = __builtin_bit_cast(float, w >= 0 && w < V ? (int)w : -1);
     }
     __syncthreads();
-    if (ty >= ty_count || q0 >= N || first >= V) return;
+    if (ty >= ty_count || mine * P >= N || first >= V) return;
     float c[P], r[P], log_s[P], gl[P], gh[P], h[P];
     int word[P]; // from the lane's first row on
 #pragma unroll
@@ -661,7 +674,14 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *L, i
                 if constexpr (decltype(words)::value) g += word[p] == (int)(v0 - first) + i ? gl[p] : 0.f;
                 o.v[p] = Logit<T>::narrow(g);
             }
-            if (i < left) *reinterpret_cast<Piece<T, P> *>(dst + i * lddl) = o;
+            if (i >= left) continue;
+            if (WHOLE || shared == 0) {
+                *reinterpret_cast<Piece<T, P> *>(dst + i * lddl) = o;
+            } else {
+#pragma unroll
+                for (int p = 1; p < P; ++p)
+                    if (p >= shared) dst[i * lddl + p] = o.v[p];
+            }
         }
     };
 #pragma unroll 1
@@ -674,9 +694,11 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *L, i
     }
 }
 
-// Columns per lane and lanes per row.  A piece of P columns is one load: P divides N and the row pitch, the base is aligned to
-// it.  Wider pieces need fewer instructions a column, and fewer lanes: they are taken while `lanes` of them with `rows` rows each
-// are left (131072: two wavefronts on every SIMD).
+// Columns per lane and lanes per row.  Wider pieces of P columns, one load each, need fewer instructions a column, and fewer lanes:
+// they are taken while `lanes` of them with `rows` rows each are left (131072: two wavefronts on every SIMD).  P divides N and
+// the row pitch and the base is aligned to it, if 8 bytes or more can be had that way; otherwise the widest at any address, the last
+// piece of a row shared with its neighbour (us, loss and gradient: 71485 words, 1877 columns f32 461 -> 403 against one column a
+// lane; 41089 words, 2561 columns f16 224 -> 187; 50000 words, 300 columns f16 40 in 16 bytes at any address, 35 in aligned 8).
 struct LpShape {
     int p, tx, ty;
     int64_t col_blocks;
@@ -686,13 +708,14 @@ static LpShape lp_shape(int es, int64_t V, int64_t N, int64_t bits, int rows, in
     LpShape s;
     s.p = 1;
     const int64_t pieces_of_rows = (V + rows - 1) / rows;
-    for (int p = most_bytes / es; p > 1; p /= 2) {
-        if (N % p != 0 || (bits & (p * es - 1)) != 0) continue;
-        if (p > least && pieces_of_rows * (N / p) < lanes) continue;
-        s.p = p;
-        break;
-    }
-    const int64_t pieces = N / s.p;
+    for (int pass = 0; pass < 2 && s.p == 1; ++pass)
+        for (int p = most_bytes / es; p > 1; p /= 2) {
+            if (pass == 0 && (p * es < 8 || N % p != 0 || (bits & (p * es - 1)) != 0)) continue;
+            if (p > N || (p > least && pieces_of_rows * ((N + p - 1) / p) < lanes)) continue;
+            s.p = p;
+            break;
+        }
+    const int64_t pieces = (N + s.p - 1) / s.p;
     // few lanes in all: workgroups of one wavefront, so that more compute units take part
     const int threads = pieces_of_rows * pieces <= 16384 ? 64 : LP_THREADS;
     s.col_blocks = (pieces + 63) / 64;
@@ -707,12 +730,12 @@ struct LpPlan {
     int64_t runs, slices, run_pitch;
     uint64_t part_bytes, bytes;
 };
-static LpPlan lp_plan(int es, int64_t V, int64_t N, int32_t top, int64_t bits)
+static LpPlan lp_plan(int es, int64_t V, int64_t N, int32_t top)
 {
     LpPlan p;
     // The top words' comparisons are hidden by more wavefronts (65536 words, 256 tokens bf16: 8-byte pieces 24.6 us, 2-byte ones
     // 22.5; 131072 words, 64 tokens 22.1 and 22.8).
-    p.shape = top > 0 ? lp_shape(es, V, N, bits, LP_RUN, 8, 1, 524288) : lp_shape(es, V, N, bits, LP_RUN, 8, 2, 131072);
+    p.shape = top > 0 ? lp_shape(es, V, N, 0, LP_RUN, 8, 1, 524288) : lp_shape(es, V, N, 0, LP_RUN, 8, 2, 131072);
     const int64_t all = (V + LP_RUN - 1) / LP_RUN;
     // runs a lane: as many as leave 2048 workgroups, eight for each compute unit
     const int64_t groups = (all + p.shape.ty - 1) / p.shape.ty * p.shape.col_blocks;
@@ -723,50 +746,48 @@ static LpPlan lp_plan(int es, int64_t V, int64_t N, int32_t top, int64_t bits)
     p.bytes = p.part_bytes + (top > 0 ? (uint64_t)p.run_pitch * (uint64_t)N * 8 : 0);
     return p;
 }
-uint64_t logprobs_workspace_bytes(int es, int64_t V, int64_t N, int32_t top)
-{
-    // whatever the alignment of the call: the pieces decide how many slices there are
-    uint64_t most = 0;
-    for (int64_t bits = es; bits <= 16; bits *= 2) {
-        const uint64_t b = lp_plan(es, V, N, top, bits).bytes;
-        most = b > most ? b : most;
-    }
-    return most;
-}
+uint64_t logprobs_workspace_bytes(int es, int64_t V, int64_t N, int32_t top) { return lp_plan(es, V, N, top).bytes; }
 
 template <typename T>
 static int launch_logprobs_t(const T *L, int64_t ldl, int64_t V, int64_t N, const int64_t *tok, float *logp, float *entropy,
                              float *stats, int32_t top, int64_t *top_ids, float *top_logp, void *ws, hipStream_t stream)
 {
-    const bool column = N == 1 && ldl == 1 && ((uintptr_t)L & 15) == 0;
+    const bool column = N == 1 && ldl == 1;
     if (column && V <= LP_COLUMN_MOST) {
         auto kern = top > 0 ? logprobs_column_kernel<T, true> : logprobs_column_kernel<T, false>;
         LRBI_LAUNCH(kern, dim3(1), dim3(LP_COLUMN_LANES), 0, stream, L, (int)V, tok, logp, entropy, stats, top, top_ids, top_logp);
         return LRBI_OK;
     }
-    const LpPlan p = lp_plan((int)sizeof(T), V, N, top, (int64_t)(uintptr_t)L | ldl * (int64_t)sizeof(T));
+    const LpPlan p = lp_plan((int)sizeof(T), V, N, top);
     float4 *part = (float4 *)ws;
     float *run_max = (float *)((char *)ws + p.part_bytes);
     uint32_t *run_more = (uint32_t *)run_max + p.run_pitch * N;
     const int threads = p.shape.tx * p.shape.ty <= 64 ? 64 : LP_THREADS, per = LP_THREADS / 64;
     const int64_t blocks = p.shape.col_blocks * p.slices, finish = (N + per - 1) / per;
     if (blocks > 0x7FFFFFFF || finish > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-#define LRBI_PASS_TOP(P, COLUMN, TOP)                                                                                               \
-    LRBI_LAUNCH((logprobs_pass_kernel<T, P, COLUMN, TOP>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N, p.shape.tx, \
-                p.shape.ty, p.shape.col_blocks, p.runs, p.slices, part, run_max, run_more, p.run_pitch)
-#define LRBI_PASS(P, COLUMN)                                                                                               \
+#define LRBI_PASS_TOP(P, WHOLE, COLUMN, TOP)                                                                               \
+    LRBI_LAUNCH((logprobs_pass_kernel<T, P, WHOLE, COLUMN, TOP>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N,  \
+                p.shape.tx, p.shape.ty, p.shape.col_blocks, p.runs, p.slices, part, run_max, run_more, p.run_pitch)
+#define LRBI_PASS(P, WHOLE, COLUMN)                                                                                        \
     do {                                                                                                                   \
-        if (top > 0) LRBI_PASS_TOP(P, COLUMN, true);                                                                       \
-        else LRBI_PASS_TOP(P, COLUMN, false);                                                                              \
+        if (top > 0) LRBI_PASS_TOP(P, WHOLE, COLUMN, true);                                                                \
+        else LRBI_PASS_TOP(P, WHOLE, COLUMN, false);                                                                       \
     } while (0)
+    const bool whole = N % p.shape.p == 0;
     switch (p.shape.p) {
     case 1:
-        if (column) LRBI_PASS(1, true);
-        else LRBI_PASS(1, false);
+        if (column) LRBI_PASS(1, true, true);
+        else LRBI_PASS(1, true, false);
         break;
-    case 2: LRBI_PASS(2, false); break;
+    case 2:
+        if (whole) LRBI_PASS(2, true, false);
+        else LRBI_PASS(2, false, false);
+        break;
     default:
-        if constexpr (sizeof(T) == 2) LRBI_PASS(4, false);
+        if constexpr (sizeof(T) == 2) {
+            if (whole) LRBI_PASS(4, true, false);
+            else LRBI_PASS(4, false, false);
+        }
         break;
     }
 #undef LRBI_PASS
@@ -804,15 +825,25 @@ static int launch_logprobs_grad_t(const T *L, int64_t ldl, int64_t V, int64_t N,
     batches = batches < 1 ? 1 : batches > 8 ? 8 : batches;
     const int64_t rows = s.ty * batches * LP_GRAD, row_blocks = (V + rows - 1) / rows, blocks = s.col_blocks * row_blocks;
     if (blocks > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-#define LRBI_GRAD(P)                                                                                                       \
-    LRBI_LAUNCH((logprobs_grad_kernel<T, P>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N, tok, stats, entropy,  \
-                g_logp, g_entropy, DL, lddl, s.tx, s.ty, s.col_blocks, batches)
+#define LRBI_GRAD(P, WHOLE)                                                                                                \
+    LRBI_LAUNCH((logprobs_grad_kernel<T, P, WHOLE>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N, tok, stats,  \
+                entropy, g_logp, g_entropy, DL, lddl, s.tx, s.ty, s.col_blocks, batches)
+    const bool whole = N % s.p == 0;
     switch (s.p) {
-    case 1: LRBI_GRAD(1); break;
-    case 2: LRBI_GRAD(2); break;
-    case 4: LRBI_GRAD(4); break;
+    case 1: LRBI_GRAD(1, true); break;
+    case 2:
+        if (whole) LRBI_GRAD(2, true);
+        else LRBI_GRAD(2, false);
+        break;
+    case 4:
+        if (whole) LRBI_GRAD(4, true);
+        else LRBI_GRAD(4, false);
+        break;
     default:
-        if constexpr (sizeof(T) == 2) LRBI_GRAD(8);
+        if constexpr (sizeof(T) == 2) {
+            if (whole) LRBI_GRAD(8, true);
+            else LRBI_GRAD(8, false);
+        }
         break;
     }
 #undef LRBI_GRAD

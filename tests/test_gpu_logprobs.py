@@ -100,6 +100,41 @@ def test_forward_and_gradient(dtype, V, N, top):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,N,top", [(20000, 431, 0), (39000, 431, 3), (131071, 301, 20), (2000, 4097, 0)])
+def test_many_odd_columns(dtype, V, N, top):
+    """Rows that no piece of several columns divides: what stands beside them stays, and the gradient may take the logits' place."""
+    print("logprobs, odd columns", dtype, V, N, top, flush=True)
+    gen = torch.Generator(device=dev()).manual_seed(V + N)
+    whole = torch.randn(V, N + 2, device=dev(), generator=gen).mul_(3).to(TORCH_DTYPE[dtype])
+    logits, tokens = whole[:, 1:1 + N], torch.randint(-1, V, (N,), device=dev(), generator=gen)
+    r = lrbi.token_logprobs(logits, tokens, top=top)
+    x = logits.double()
+    lp = torch.log_softmax(x, 0)
+    p = lp.exp()
+    H = -(p * lp).sum(0)
+    own = torch.where(tokens < 0, 0, lp.gather(0, tokens.clamp(min=0)[None])[0])
+    tol = 3e-5 + 2.0 ** -22 * lp.abs().max()  # as in _check
+    assert ((r.logp - own).abs() <= tol).all() and ((r.entropy - H).abs() <= 3e-5 * (1 + math.log(V))).all()
+    assert torch.equal(r.stats[0].double(), x.max(0).values)
+    if top:
+        order = torch.sort(x, dim=0, descending=True, stable=True)
+        assert torch.equal(r.top_ids, order.indices[:top]) and ((r.top_logp - lp.gather(0, r.top_ids)).abs() <= tol).all()
+        del order
+    gl, gh = (torch.randn(N, device=dev(), generator=gen) for _ in range(2))
+    want = torch.zeros_like(lp).scatter_(0, tokens.clamp(min=0)[None], torch.where(tokens < 0, 0.0, gl).double()[None])
+    gl64, gh64 = torch.where(tokens < 0, 0.0, gl).double(), gh.double()
+    want -= p * (gl64 + gh64 * (lp + H))
+    tol = HALF[dtype] * want.abs() + 2e-5 * p * (gl64.abs() + gh64.abs() * (lp.abs() + H + 2 + math.log(V))) + TINY[dtype]  # as in _grad_check
+    out = torch.full((V, N + 2), 7.0, device=dev()).to(TORCH_DTYPE[dtype])
+    lrbi.token_logprobs_grad(logits, tokens, r, gl, gh, out=out[:, 1:1 + N])
+    assert ((out[:, 1:1 + N].double() - want).abs() <= tol).all()
+    assert (out[:, 0] == 7).all() and (out[:, -1] == 7).all()
+    before = whole[:, [0, -1]].clone()
+    lrbi.token_logprobs_grad(logits, tokens, r, gl, gh, out=logits)
+    assert torch.equal(whole[:, 1:1 + N], out[:, 1:1 + N]) and torch.equal(whole[:, [0, -1]], before)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_strided_logits(dtype):
     """Row pitches and first columns of every alignment; the gradient in the logits' own place."""
     print("logprobs, strides", dtype, flush=True)
