@@ -13,7 +13,8 @@
 //
 // From an activation checkpoint (8-bit codes, a scale per 32 batch columns: one slab) X is staged as it is stored, 8 KB a slab, and
 // widened between the LDS read and the products, four instructions for the eight codes of two matrix instructions.  The scale
-// bytes of eight slabs at a time go to LDS the same way, two sets in turn.
+// bytes of eight slabs at a time go to LDS the same way, two sets in turn.  8192 x 8192, batch 1024 bf16 152 us = 0.90 PFLOP/s (a
+// library's product of these sizes from bf16, without mask and checkpoint: 117 us, 1.17).
 #include "lrbi_internal.hpp"
 #include "lrbi_lds_dma.hpp"
 #include "lrbi_mfma_common.hpp"
