@@ -274,11 +274,10 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__re
 }
 
 static constexpr int LP_LIST = 256;  // words a wavefront holds at a time
-static constexpr int LP_ROUND = 2048; // runs it looks at in a round: eight loads of four a lane, in flight together
-static constexpr int LP_AHEAD = LP_ROUND / 256;
-struct alignas(16) LpList {
+// It looks at 256 AHEAD runs in a round: AHEAD loads of four a lane, in flight together.
+template <int AHEAD> struct alignas(16) LpList {
     uint64_t key[LP_LIST + 8]; // larger: the likelier word; all different
-    int run[LP_ROUND], again[64];
+    int run[256 * AHEAD], again[64];
 };
 // a logit's place among the numbers (both zeros the same), then the lower word first
 __device__ __forceinline__ uint64_t lp_key(float x, int word)
@@ -295,7 +294,7 @@ __device__ __forceinline__ int lp_key_word(uint64_t key) { return (int)~(uint32_
 
 // The K largest keys of the list, sorted, at its start; the rest is dropped.  Returns how many there are.  A key's place is the
 // number of keys above it; PER keys a lane.
-template <int PER> __device__ __forceinline__ int lp_rank_of(LpList &l, int count, int K, int lane)
+template <int PER, int AHEAD> __device__ __forceinline__ int lp_rank_of(LpList<AHEAD> &l, int count, int K, int lane)
 {
     wave_fence();
     if (lane < 8) l.key[count + lane] = 0; // below every key
@@ -323,7 +322,7 @@ template <int PER> __device__ __forceinline__ int lp_rank_of(LpList &l, int coun
     wave_fence();
     return count < K ? count : K;
 }
-__device__ __forceinline__ int lp_rank(LpList &l, int count, int K, int lane)
+template <int AHEAD> __device__ __forceinline__ int lp_rank(LpList<AHEAD> &l, int count, int K, int lane)
 {
     return count <= 64 ? lp_rank_of<1>(l, count, K, lane) : lp_rank_of<LP_LIST / 64>(l, count, K, lane);
 }
@@ -342,19 +341,21 @@ __device__ __forceinline__ void lp_runs(float (&p)[4], const float *run_max, int
 // The K most likely words of column q, by one wavefront: sorted in `l`; returns how many there are (words at -infinity are
 // none, nor are NaN).  run_max: the column's runs, 16-byte aligned, room for a multiple of 4; piece: the first round of them,
 // run 256 k + 4 lane + e as piece[k][e].
-template <typename T>
-__device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_t ldl, int V, int64_t q, const float *__restrict__ run_max,
-                                      const uint32_t *__restrict__ run_more, int runs, float (&piece)[LP_AHEAD][4], int K, int lane)
+template <typename T, int AHEAD>
+__device__ __forceinline__ int lp_top(LpList<AHEAD> &l, const T *__restrict__ L, int64_t ldl, int V, int64_t q, const float *__restrict__ run_max,
+                                      const uint32_t *__restrict__ run_more, int runs, float (&piece)[AHEAD][4], int K, int lane)
 {
+    constexpr int ROUND = 256 * AHEAD;
+    typedef std::conditional_t<(AHEAD > 8), uint64_t, uint32_t> Hits; // a bit a run of the lane's
     const float none = -__builtin_inff();
     float mine = none;
     for (int i0 = 0;;) {
 #pragma unroll
-        for (int k = 0; k < LP_AHEAD; ++k) mine = fmaxf(mine, fmaxf(fmaxf(piece[k][0], piece[k][1]), fmaxf(piece[k][2], piece[k][3])));
-        i0 += LP_ROUND;
+        for (int k = 0; k < AHEAD; ++k) mine = fmaxf(mine, fmaxf(fmaxf(piece[k][0], piece[k][1]), fmaxf(piece[k][2], piece[k][3])));
+        i0 += ROUND;
         if (i0 >= runs) break;
 #pragma unroll
-        for (int k = 0; k < LP_AHEAD; ++k) lp_runs(piece[k], run_max, i0 + 256 * k + 4 * lane, runs);
+        for (int k = 0; k < AHEAD; ++k) lp_runs(piece[k], run_max, i0 + 256 * k + 4 * lane, runs);
     }
     // a bound that K lanes' maxima reach: the largest number of 16 leading bits for which that holds
     const uint32_t place = (uint32_t)(lp_key(mine, -1) >> 32);
@@ -379,16 +380,16 @@ __device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_
             if (count == K) bound = l.key[K - 1];
         }
     };
-    for (int i0 = 0; i0 < runs; i0 += LP_ROUND) {
+    for (int i0 = 0; i0 < runs; i0 += ROUND) {
         // the runs that reach the bound: each lane's behind those of the lanes before it
-        uint32_t hit = 0;
+        Hits hit = 0;
 #pragma unroll
-        for (int k = 0; k < LP_AHEAD; ++k) {
-            if (runs > LP_ROUND) lp_runs(piece[k], run_max, i0 + 256 * k + 4 * lane, runs); // otherwise they are there
+        for (int k = 0; k < AHEAD; ++k) {
+            if (runs > ROUND) lp_runs(piece[k], run_max, i0 + 256 * k + 4 * lane, runs); // otherwise they are there
 #pragma unroll
-            for (int e = 0; e < 4; ++e) hit |= piece[k][e] >= least && piece[k][e] > none ? 1u << (4 * k + e) : 0u;
+            for (int e = 0; e < 4; ++e) hit |= piece[k][e] >= least && piece[k][e] > none ? (Hits)1 << (4 * k + e) : 0;
         }
-        int end = __builtin_popcount(hit);
+        int end = __builtin_popcountll(hit);
 #pragma unroll
         for (int step = 1; step < 64; step *= 2) {
             const int before = __shfl_up(end, step, 64);
@@ -396,8 +397,8 @@ __device__ __forceinline__ int lp_top(LpList &l, const T *__restrict__ L, int64_
         }
         const int found = __builtin_amdgcn_readlane(end, 63);
         wave_fence();
-        for (int at = end - __builtin_popcount(hit); hit; hit &= hit - 1) {
-            const int bit = __builtin_ctz(hit);
+        for (int at = end - __builtin_popcountll(hit); hit; hit &= hit - 1) {
+            const int bit = __builtin_ctzll(hit);
             l.run[at++] = i0 + 256 * (bit >> 2) + 4 * lane + (bit & 3);
         }
         wave_fence();
@@ -458,7 +459,8 @@ template <typename T> __device__ __forceinline__ LpSums lp_join_lanes(LpSums a, 
         a = lp_join<T>(a, LpSums{__shfl_xor(a.m, step, 64), __shfl_xor(a.s, step, 64), __shfl_xor(a.t, step, 64)});
     return a;
 }
-__device__ __forceinline__ void lp_write_top(const LpList &l, int count, const LpSums &a, float ln_s, int64_t q, int64_t N, int K,
+template <int AHEAD>
+__device__ __forceinline__ void lp_write_top(const LpList<AHEAD> &l, int count, const LpSums &a, float ln_s, int64_t q, int64_t N, int K,
                                              int64_t *__restrict__ top_ids, float *__restrict__ top_logp, int lane)
 {
     if (lane < K) {
@@ -467,24 +469,28 @@ __device__ __forceinline__ void lp_write_top(const LpList &l, int count, const L
     }
 }
 
-// Joins a column's slices and writes its results, one wavefront a column.
-template <typename T, bool TOP>
-__global__ __launch_bounds__(LP_THREADS) void logprobs_finish_kernel(
+// Joins a column's slices and writes its results, one wavefront a column and workgroup: few columns go to as many compute units (four
+// wavefronts a workgroup: 94272 words, 66 tokens, 17 top words 21.9 us against 20.8, both kernels).
+// AHEAD: 0 without top words, otherwise as many as its runs fill in one round, up to 16 (us, 65536 words and below with 8, more
+// with 16 against 8: 94272 words, 66 tokens, 17 top words 21.2 -> 17.3; 131072 words, one token 14.4 -> 11.8).
+template <typename T, int AHEAD>
+__global__ __launch_bounds__(64) void logprobs_finish_kernel(
     const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N, const int64_t *__restrict__ tok, const float4 *__restrict__ part,
     int64_t slices, const float *__restrict__ run_max, const uint32_t *__restrict__ run_more, int64_t run_pitch, float *__restrict__ logp,
     float *__restrict__ entropy, float *__restrict__ stats, int K, int64_t *__restrict__ top_ids, float *__restrict__ top_logp)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t q = wide_block() * (LP_THREADS / 64) + wave;
-    if (q >= N) return; // whole wavefronts; no barrier below
+    constexpr bool TOP = AHEAD > 0;
+    const int lane = threadIdx.x;
+    const int64_t q = wide_block();
+    if (q >= N) return;
     // what the column needs is asked for at once: its word, the first round of its runs, its slices
     const int64_t word = logp ? tok[q] : -1;
     const int runs = (int)((V + LP_RUN - 1) / LP_RUN);
     const float *column_runs = TOP ? run_max + q * run_pitch : nullptr;
-    float piece[LP_AHEAD][4];
+    float piece[TOP ? AHEAD : 1][4];
     if constexpr (TOP)
 #pragma unroll
-        for (int k = 0; k < LP_AHEAD; ++k) lp_runs(piece[k], column_runs, 256 * k + 4 * lane, runs);
+        for (int k = 0; k < AHEAD; ++k) lp_runs(piece[k], column_runs, 256 * k + 4 * lane, runs);
     LpSums a = lp_empty<T>();
     for (int64_t i0 = 0; i0 < slices; i0 += 64 * 4) {
         float4 p[4];
@@ -501,8 +507,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_finish_kernel(
     a = lp_join_lanes<T>(a, 64);
     const float ln_s = lp_write<T>(a, q, V, N, word, x, logp != nullptr, logp, entropy, stats, lane);
     if constexpr (TOP) {
-        __shared__ LpList lists[LP_THREADS / 64];
-        LpList &l = lists[wave];
+        __shared__ LpList<AHEAD> l;
         const int count = lp_top(l, L, ldl, (int)V, q, column_runs, run_more + q * run_pitch, runs, piece, K, lane);
         lp_write_top(l, count, a, ln_s, q, N, K, top_ids, top_logp, lane);
     }
@@ -595,16 +600,17 @@ __global__ __launch_bounds__(LP_COLUMN_LANES) void logprobs_column_kernel(const 
     a = lp_join_lanes<T>(join[lane & 15], 16);
     const float ln_s = lp_write<T>(a, 0, V, 1, word, own, logp != nullptr, logp, entropy, stats, lane);
     if constexpr (TOP) {
-        __shared__ LpList l;
+        constexpr int AHEAD = LP_COLUMN_MOST / LP_RUN / 256; // one round
+        __shared__ LpList<AHEAD> l;
         const int runs = (V + LP_RUN - 1) / LP_RUN;
-        float piece[LP_AHEAD][4];
+        float piece[AHEAD][4];
 #pragma unroll
-        for (int k = 0; k < LP_AHEAD; ++k) lp_runs(piece[k], run_max, 256 * k + 4 * lane, runs);
+        for (int k = 0; k < AHEAD; ++k) lp_runs(piece[k], run_max, 256 * k + 4 * lane, runs);
         const int count = lp_top(l, L, 1, V, 0, run_max, run_more, runs, piece, K, lane);
         lp_write_top(l, count, a, ln_s, 0, 1, K, top_ids, top_logp, lane);
     }
 }
-static_assert(LP_COLUMN_LANES == 16 * 64 && LP_COLUMN_MOST / LP_RUN <= LP_ROUND, "one partial a lane of 16, one round of runs");
+static_assert(LP_COLUMN_LANES == 16 * 64 && LP_COLUMN_MOST % (256 * LP_RUN) == 0, "one partial a lane of 16, one round of runs");
 
 // dx_v = gl (1[v = word] - p_v) - gh p_v (log p_v + entropy); a lane owns P columns and the `batches` batches of 8 rows from
 // ((block * ty_count) + ty) * batches on.  DL may be L: a batch is read whole before any of it is
@@ -766,9 +772,9 @@ static int launch_logprobs_t(const T *L, int64_t ldl, int64_t V, int64_t N, cons
     float4 *part = (float4 *)ws;
     float *run_max = (float *)((char *)ws + p.part_bytes);
     uint32_t *run_more = (uint32_t *)run_max + p.run_pitch * N;
-    const int threads = p.shape.tx * p.shape.ty <= 64 ? 64 : LP_THREADS, per = LP_THREADS / 64;
-    const int64_t blocks = p.shape.col_blocks * p.slices, finish = (N + per - 1) / per;
-    if (blocks > 0x7FFFFFFF || finish > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
+    const int threads = p.shape.tx * p.shape.ty <= 64 ? 64 : LP_THREADS;
+    const int64_t blocks = p.shape.col_blocks * p.slices;
+    if (blocks > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
 #define LRBI_PASS_TOP(P, WHOLE, COLUMN, TOP)                                                                               \
     LRBI_LAUNCH((logprobs_pass_kernel<T, P, WHOLE, COLUMN, TOP>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N,  \
                 p.shape.tx, p.shape.ty, p.shape.col_blocks, p.runs, p.slices, part, run_max, run_more, p.run_pitch)
@@ -796,11 +802,13 @@ static int launch_logprobs_t(const T *L, int64_t ldl, int64_t V, int64_t N, cons
     }
 #undef LRBI_PASS
 #undef LRBI_PASS_TOP
-#define LRBI_FINISH(TOP)                                                                                                   \
-    LRBI_LAUNCH((logprobs_finish_kernel<T, TOP>), wide_grid(finish, LP_THREADS), dim3(LP_THREADS), 0, stream, L, ldl, V, N, tok, part,  \
+#define LRBI_FINISH(AHEAD)                                                                                                   \
+    LRBI_LAUNCH((logprobs_finish_kernel<T, AHEAD>), wide_grid(N, 64), dim3(64), 0, stream, L, ldl, V, N, tok, part,  \
                 p.slices, run_max, run_more, p.run_pitch, logp, entropy, stats, top, top_ids, top_logp)
-    if (top > 0) LRBI_FINISH(true);
-    else LRBI_FINISH(false);
+    if (top == 0) LRBI_FINISH(0);
+    else if (V <= 256 * 4 * LP_RUN) LRBI_FINISH(4);
+    else if (V <= 256 * 8 * LP_RUN) LRBI_FINISH(8);
+    else LRBI_FINISH(16);
 #undef LRBI_FINISH
     return LRBI_OK;
 }

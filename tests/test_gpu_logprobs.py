@@ -134,6 +134,18 @@ def test_many_odd_columns(dtype, V, N, top):
     assert torch.equal(whole[:, 1:1 + N], out[:, 1:1 + N]) and torch.equal(whole[:, [0, -1]], before)
 
 
+@pytest.mark.parametrize("V", [20000, 32769, 65537, 131072, 150000])
+def test_top_words_of_large_vocabularies(V):
+    """Several rounds of runs, every run in the list, the top words at the end of the last round."""
+    print("logprobs, large vocabulary", V, flush=True)
+    x = torch.zeros(V, 3, device=dev(), dtype=torch.float16)  # all equal: the lowest words
+    x[:, 1] = torch.arange(V, device=dev()).sub(V).mul(2.0 ** -4).clamp(min=-2000.0).half()  # towards the end larger, in groups
+    x[:, 2] = torch.randn(V, generator=torch.Generator().manual_seed(V)).half().to(dev())
+    for N in (1, 3):
+        r = lrbi.token_logprobs(x[:, 3 - N:], None, top=64)
+        assert torch.equal(r.top_ids, torch.sort(x[:, 3 - N:], dim=0, descending=True, stable=True).indices[:64])
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_strided_logits(dtype):
     """Row pitches and first columns of every alignment; the gradient in the logits' own place."""
