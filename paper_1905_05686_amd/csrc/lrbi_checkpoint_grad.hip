@@ -366,9 +366,10 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
 }
 
 // The same for few blocks: 64 x 64 of dW a workgroup, slabs of 128 batch columns, a quarter of which each wavefront multiplies; the
-// four sums are added in LDS.  Bound by the chain of a slab's loads, its products and two barriers: four times the workgroups, half the
-// slabs (us against the kernel above: 6793 x 203, batch 896 f16 27.6 -> 15.2; 362 x 1088, batch 557 f16 17 -> 9.4; 192 x 1088, batch 150
-// f32 18 -> 9.4; with 256 blocks of 128 x 128 it would take 12.5 instead of 9.5).
+// four sums are added in LDS.  Bound by a slab's chain of loads, two barriers and products, so two slabs are on their way: four times the
+// workgroups, half the slabs (us against the kernel above: 6793 x 203, batch 896 f16 27.6 -> 14.6; 362 x 1088, batch 557 f16 17 -> 9.4;
+// 192 x 1088, batch 150 f32 18 -> 9.4; with 256 blocks of 128 x 128 it would take 12.5 instead of 9.5.  One slab under way: 256 x 256,
+// batch 16384 bf16 124 instead of 96.  Operands straight from memory into the lanes, no LDS: 22 instead of 15 on the first).
 static constexpr int CS_B = 64, CS_K = 128;
 static constexpr int CS_A_ROW = CS_K + 8;  // halfs
 static constexpr int CS_X_ROW = CS_K + 16; // bytes
@@ -406,25 +407,28 @@ __global__ __launch_bounds__(CG_THREADS, 2) void checkpoint_grad_small_kernel(Ge
 
     // lane = (row tid / 16 + 16 c, eight columns tid % 16) of dY, (row tid / 8 + 32 c, 16 columns tid % 8) of X
     constexpr int AV = sizeof(E) / 2;
-    uint4 areg[4][AV], xreg[2];
-    uint32_t sreg[2];
-    auto load = [&](int slab) __attribute__((always_inline)) {
+    struct Slab {
+        uint4 a[4][AV], x[2];
+        uint32_t s[2];
+    } w0, w1; // two on their way
+    auto load = [&](Slab &w, int slab) __attribute__((always_inline)) {
         const int q = slab * CS_K + (tid & 15) * 8;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int64_t i = i0 + (tid >> 4) + 16 * c, row = i < g.m ? i : g.m - 1; // (rows past the matrix are not stored)
 #pragma unroll
-            for (int k = 0; k < AV; ++k) areg[c][k] = cg_load(DY + row * lddy, q + k * (16 / (int)sizeof(E)), N);
+            for (int k = 0; k < AV; ++k) w.a[c][k] = cg_load(DY + row * lddy, q + k * (16 / (int)sizeof(E)), N);
         }
         const int p = cg_piece(slab * CS_K + (tid & 7) * 16, N);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int64_t j = j0 + (tid >> 3) + 32 * c, row = j < g.n ? j : g.n - 1;
-            xreg[c] = *reinterpret_cast<const uint4 *>(X + row * ldx + p);
-            sreg[c] = XS[row * ldxs + (p >> 5)];
+            w.x[c] = *reinterpret_cast<const uint4 *>(X + row * ldx + p);
+            w.s[c] = XS[row * ldxs + (p >> 5)];
         }
     };
-    load(0);
+    load(w0, 0);
+    if (nslabs > 1) load(w1, 1);
     CgMask q = {};
     if (wave == 0) q = cg_mask_begin(g, Ip, Iz, i0, j0, lined_up, lane);
     f32x16 acc[2][2];
@@ -434,26 +438,25 @@ __global__ __launch_bounds__(CG_THREADS, 2) void checkpoint_grad_small_kernel(Ge
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
-#pragma unroll 1
-    for (int s = 0; s < nslabs; ++s) {
+    auto slab = [&](Slab &w, int s) __attribute__((always_inline)) {
         if (s) __syncthreads(); // the slab before has been read
         if ((s + 1) * CS_K > N) { // the last slab: columns behind N are zero
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int k = 0; k < AV; ++k)
-                    areg[c][k] = cg_trim<E>(areg[c][k], s * CS_K + (tid & 15) * 8 + k * (16 / (int)sizeof(E)), N);
+                    w.a[c][k] = cg_trim<E>(w.a[c][k], s * CS_K + (tid & 15) * 8 + k * (16 / (int)sizeof(E)), N);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) xreg[c] = cg_trim_codes(xreg[c], s * CS_K + (tid & 7) * 16, N);
+            for (int c = 0; c < 2; ++c) w.x[c] = cg_trim_codes(w.x[c], s * CS_K + (tid & 7) * 16, N);
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             unsigned char *dst = smem + ((tid >> 4) + 16 * c) * (CS_A_ROW * 2) + (tid & 15) * 16;
             if constexpr (PARTS == 1) {
-                *reinterpret_cast<uint4 *>(dst) = areg[c][0];
+                *reinterpret_cast<uint4 *>(dst) = w.a[c][0];
             } else {
                 uint4 parts[3];
-                cg_split(areg[c], parts);
+                cg_split(w.a[c], parts);
 #pragma unroll
                 for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4 *>(dst + k * S::a_bytes) = parts[k];
             }
@@ -461,12 +464,12 @@ __global__ __launch_bounds__(CG_THREADS, 2) void checkpoint_grad_small_kernel(Ge
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int row = (tid >> 3) + 32 * c;
-            *reinterpret_cast<uint4 *>(smem + S::x_off + row * CS_X_ROW + (tid & 7) * 16) = xreg[c];
-            if ((tid & 1) == 0) *reinterpret_cast<uint32_t *>(smem + S::s_off + row * 16 + ((tid >> 1) & 3) * 4) = sreg[c] << 23;
+            *reinterpret_cast<uint4 *>(smem + S::x_off + row * CS_X_ROW + (tid & 7) * 16) = w.x[c];
+            if ((tid & 1) == 0) *reinterpret_cast<uint32_t *>(smem + S::s_off + row * 16 + ((tid >> 1) & 3) * 4) = w.s[c] << 23;
         }
-        if (s + 1 < nslabs) load(s + 1);
+        if (s + 2 < nslabs) load(w, s + 2);
         __syncthreads();
-        if (s * CS_K + wave * 32 >= N) continue; // nothing in this quarter
+        if (s * CS_K + wave * 32 >= N) return; // nothing in this quarter
         const unsigned char *as = smem + l32 * (CS_A_ROW * 2) + wave * 64 + 16 * lg;
         const unsigned char *xs = smem + S::x_off + l32 * CS_X_ROW + wave * 32 + 8 * lg;
         float sc[2];
@@ -488,6 +491,11 @@ __global__ __launch_bounds__(CG_THREADS, 2) void checkpoint_grad_small_kernel(Ge
                     for (int b = 0; b < 2; ++b) acc[a][b] = mfma_32x32x16(Op{}, xf[a], yf[b], acc[a][b]);
             }
         }
+    };
+#pragma unroll 1
+    for (int s = 0; s < nslabs; s += 2) {
+        slab(w0, s);
+        if (s + 1 < nslabs) slab(w1, s + 1);
     }
     __syncthreads(); // the last slab has been read: the sums take its place
     float *sums = (float *)smem + wave * (CS_B * CS_P_ROW);
