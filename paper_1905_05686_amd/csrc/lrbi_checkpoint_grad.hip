@@ -10,11 +10,11 @@
 //   * fp32 dY is split into three bf16 parts, y = y1 + y2 + y3 exactly; a checkpoint's values are bf16 numbers, so three 16-bit
 //     products, exact in fp32, do the work of sixteen times slower fp32 ones.
 //   * output: f16 / bf16 through LDS, eight rows of 128 bytes a store; fp32 with the roles of the two operands exchanged, so that a
-//     store is two rows of 128 bytes (2324 x 4839, batch 211: 63 -> 47 us).
+//     store is two rows of 128 bytes (2324 x 4839, batch 211: 63 -> 40 us).
 //   * mask: tile sizes that are multiples of 64 and ranks up to 64: each wavefront fetches its block's slices of the factors before
 //     the products and forms its words behind them (Eq. 3); other shapes word by word.
 // 4100 x 9224, batch 131 f16 36 to 39 us (its 75 MB written alone 14), batch 40 23, batch 192 37: 16 and 7 more for each slab; 4096 x 4096,
-// batch 100 f32 34; 2000 x 8000 in 300 x 320 tiles, batch 777 f16 55.  With stores, loads or products left out (4096 x 9216, batch 128, 27 us)
+// batch 100 f32 29; 2000 x 8000 in 300 x 320 tiles, batch 777 f16 55.  With stores, loads or products left out (4096 x 9216, batch 128, 27 us)
 // 21, 23, 23: three workgroups a compute unit in turns of loading, multiplying and storing, no one of which is full.
 #include <type_traits>
 
@@ -347,20 +347,31 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
                 }
             }
         } else { // the lane holds column l32 and rows 8 * (v / 4) + 4 * lg + (v % 4): a store is two rows of 128 bytes
+            // Stores count with the loads, in order: a block that lies inside has no branches here, so that the wait for the next slab
+            // can leave its stores on their way (4096 x 4096, batch 131: 41 -> 36.5 us; f16 / bf16, with an eighth of the stores: nothing).
+            auto output = [&](auto inside_c) __attribute__((always_inline)) {
+                constexpr bool inside = decltype(inside_c)::value;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int rr = b * 32 + 8 * (v >> 2) + (v & 3);
-                    const int64_t i = i0 + rr + 4 * lg;
-                    if (i >= g.m) continue;
-                    E *dst = DW + i * lddw + j0 + l32;
+                    for (int v = 0; v < 16; ++v) {
+                        const int rr = b * 32 + 8 * (v >> 2) + (v & 3);
+                        const int64_t i = i0 + rr + 4 * lg;
+                        if (!inside && i >= g.m) continue;
+                        E *dst = DW + i * lddw + j0 + l32;
 #pragma unroll
-                    for (int a = 0; a < 2; ++a) {
-                        const uint32_t lo = __builtin_amdgcn_readlane(words[a], rr), hi = __builtin_amdgcn_readlane(words[a], rr + 4);
-                        if (j0 + a * 32 + l32 < g.n) dst[a * 32] = ((lg ? hi : lo) >> l32 & 1u) ? acc[a][b][v] : 0.f;
+                        for (int a = 0; a < 2; ++a) {
+                            const uint32_t lo = __builtin_amdgcn_readlane(words[a], rr), hi = __builtin_amdgcn_readlane(words[a], rr + 4);
+                            if (inside || j0 + a * 32 + l32 < g.n) dst[a * 32] = ((lg ? hi : lo) >> l32 & 1u) ? acc[a][b][v] : 0.f;
+                        }
                     }
-                }
+            };
+            if (i0 + 64 <= g.m && j0 + 64 <= g.n) {
+                output(std::true_type{});
+            } else {
+                output(std::false_type{});
+                __builtin_amdgcn_s_waitcnt(0x0F70); // every load and store, so that the other path's count holds behind both
+            }
         }
     }
 }
