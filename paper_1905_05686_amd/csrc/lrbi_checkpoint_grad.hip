@@ -176,7 +176,7 @@ __device__ __forceinline__ void cg_mask_end(CgMask &q, uint32_t *fz, bool lined_
         }
 }
 
-template <typename Tag>
+template <typename Tag, bool STREAM>
 __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_grad_kernel(Geom g, const typename CgTypes<Tag>::elem *__restrict__ DY, int64_t lddy,
                                                                      const unsigned char *__restrict__ X, int64_t ldx,
                                                                      const unsigned char *__restrict__ XS, int64_t ldxs, int N,
@@ -337,7 +337,8 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
                         struct __attribute__((packed, aligned(2))) Piece { // at any element's address
                             uint32_t x, y, z, w;
                         };
-                        *reinterpret_cast<Piece *>(dst) = {v.x, v.y, v.z, v.w};
+                        if constexpr (STREAM) stream_store16(dst, v);
+                        else *reinterpret_cast<Piece *>(dst) = {v.x, v.y, v.z, v.w};
                     } else {
                         const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -362,7 +363,9 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
 #pragma unroll
                         for (int a = 0; a < 2; ++a) {
                             const uint32_t lo = __builtin_amdgcn_readlane(words[a], rr), hi = __builtin_amdgcn_readlane(words[a], rr + 4);
-                            if (inside || j0 + a * 32 + l32 < g.n) dst[a * 32] = ((lg ? hi : lo) >> l32 & 1u) ? acc[a][b][v] : 0.f;
+                            const float value = ((lg ? hi : lo) >> l32 & 1u) ? acc[a][b][v] : 0.f;
+                            if constexpr (inside && STREAM) __builtin_nontemporal_store(value, dst + a * 32);
+                            else if (inside || j0 + a * 32 + l32 < g.n) dst[a * 32] = value;
                         }
                     }
             };
@@ -581,7 +584,10 @@ static int launch_t(const Geom &g, const void *dDY, int64_t lddy, const void *dC
         return LRBI_OK;
     }
     const int64_t groups = blocks < at_once ? blocks : at_once;
-    auto kern = checkpoint_grad_kernel<Tag>;
+    // dW past the last-level cache where it does not fit it and its rows are whole lines (16384 x 16384, batch 64 bf16 137 -> 111 us; rows
+    // that begin inside a line, 4100 x 9224: 23 -> 42)
+    const bool stream_dw = g.m * g.n * (int64_t)sizeof(E) >= LRBI_STREAM_BYTES && (((uintptr_t)dDW | (uint64_t)(lddw * (int64_t)sizeof(E))) & 127) == 0;
+    auto kern = stream_dw ? checkpoint_grad_kernel<Tag, true> : checkpoint_grad_kernel<Tag, false>;
     LRBI_SET_MAX_LDS(kern, SmemCg<Tag>::bytes);
     LRBI_LAUNCH(kern, dim3((unsigned)groups), dim3(CG_THREADS), SmemCg<Tag>::bytes, stream, g, (const E *)dDY, lddy, (const unsigned char *)dCodes,
                 ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, jblocks, blocks);

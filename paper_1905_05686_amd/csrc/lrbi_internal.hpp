@@ -282,6 +282,20 @@ inline int compute_units_of(hipStream_t stream)
 // Device helpers for Eq. 3 on packed factors.
 // ---------------------------------------------------------------------------
 
+// Loads and stores past the caches' usual order, for what is read once or written and does not fit the last-level cache (256 MB), so
+// that it cannot wait there for the next call either.  16 bytes at any 16-bit element's address.
+static constexpr int64_t LRBI_STREAM_BYTES = (int64_t)256 << 20;
+typedef uint32_t stream_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ uint4 stream_load16(const void *p)
+{
+    const stream_u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const stream_u32x4 *>(p));
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void stream_store16(void *p, uint4 v)
+{
+    __builtin_nontemporal_store(stream_u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<stream_u32x4 *>(p));
+}
+
 // LDS handed between the lanes of one wavefront: its operations complete in order, the compiler keeps theirs
 __device__ __forceinline__ void wave_fence()
 {

@@ -110,9 +110,20 @@ template <typename T> __device__ __forceinline__ LpSums lp_join(LpSums a, LpSums
     return a;
 }
 
+template <int BYTES> struct StreamWord;
+template <> struct StreamWord<2> {
+    typedef uint16_t type;
+};
+template <> struct StreamWord<4> {
+    typedef uint32_t type __attribute__((aligned(2)));
+};
+template <> struct StreamWord<8> {
+    typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2)));
+};
+
 // Rows of P columns from `src` on, rows ldl apart; COLUMN: the logits are one column without gaps (P = 1), read as
-// 16-byte pieces.
-template <typename T, int P, bool COLUMN, int ROWS>
+// 16-byte pieces.  STREAM: they are too many for the last-level cache.
+template <typename T, int P, bool COLUMN, bool STREAM, int ROWS>
 __device__ __forceinline__ void lp_load(Piece<T, P> (&x)[ROWS], const T *src, int64_t ldl, int left)
 {
     if (left < ROWS) { // past the last row: words of probability 0
@@ -131,6 +142,13 @@ __device__ __forceinline__ void lp_load(Piece<T, P> (&x)[ROWS], const T *src, in
 #pragma unroll
         for (int i = 0; i < N16; ++i) v[i] = reinterpret_cast<const Piece16<T> *>(src)[i];
         __builtin_memcpy(x, v, sizeof(x));
+    } else if constexpr (STREAM) {
+        typedef typename StreamWord<P * sizeof(T)>::type Word;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const Word w = __builtin_nontemporal_load(reinterpret_cast<const Word *>(src + i * ldl));
+            __builtin_memcpy(&x[i], &w, sizeof(w));
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) x[i] = *reinterpret_cast<const Piece<T, P> *>(src + i * ldl);
@@ -149,7 +167,7 @@ __device__ __forceinline__ float lp_second(uint32_t more) { return __builtin_bit
 
 // One pass: lane (tx, ty) of a workgroup takes columns (block * tx_count + tx) P .. + P - 1 and the `runs` runs of 32 rows
 // from ((slice * ty_count) + ty) * runs on.  part: [column][slice]; TOP: run_max, run_more: [column][run_pitch].
-template <typename T, int P, bool WHOLE, bool COLUMN, bool TOP>
+template <typename T, int P, bool WHOLE, bool COLUMN, bool TOP, bool STREAM>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N,
                                                                    int tx_count, int ty_count, int64_t col_blocks, int64_t runs, int64_t slices,
                                                                    float4 *__restrict__ part, float *__restrict__ run_max,
@@ -185,7 +203,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_pass_kernel(const T *__re
                 if (v0 >= V) break;
                 const int left = V - v0 < LP_BATCH ? (int)(V - v0) : LP_BATCH;
                 Piece<T, P> x[LP_BATCH];
-                lp_load<T, P, COLUMN, LP_BATCH>(x, L + v0 * ldl + q0, ldl, left);
+                lp_load<T, P, COLUMN, STREAM, LP_BATCH>(x, L + v0 * ldl + q0, ldl, left);
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     float b = Logit<T>::widen(x[0].v[p]);
@@ -671,7 +689,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_grad_kernel(const T *L, i
     const auto batch = [&](int64_t v0, auto words) {
         const int left = V - v0 < LP_GRAD ? (int)(V - v0) : LP_GRAD;
         Piece<T, P> x[LP_GRAD];
-        lp_load<T, P, false, LP_GRAD>(x, L + v0 * ldl + q0, ldl, left);
+        lp_load<T, P, false, false, LP_GRAD>(x, L + v0 * ldl + q0, ldl, left);
         T *dst = DL + v0 * lddl + q0;
 #pragma unroll
         for (int i = 0; i < LP_GRAD; ++i) {
@@ -775,15 +793,19 @@ static int launch_logprobs_t(const T *L, int64_t ldl, int64_t V, int64_t N, cons
     const int threads = p.shape.tx * p.shape.ty <= 64 ? 64 : LP_THREADS;
     const int64_t blocks = p.shape.col_blocks * p.slices;
     if (blocks > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-#define LRBI_PASS_TOP(P, WHOLE, COLUMN, TOP)                                                                               \
-    LRBI_LAUNCH((logprobs_pass_kernel<T, P, WHOLE, COLUMN, TOP>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, N,  \
-                p.shape.tx, p.shape.ty, p.shape.col_blocks, p.runs, p.slices, part, run_max, run_more, p.run_pitch)
+#define LRBI_PASS_TOP(P, WHOLE, COLUMN, TOP, STREAM)                                                                       \
+    LRBI_LAUNCH((logprobs_pass_kernel<T, P, WHOLE, COLUMN, TOP, STREAM>), wide_grid(blocks, threads), dim3(threads), 0, stream, L, ldl, V, \
+                N, p.shape.tx, p.shape.ty, p.shape.col_blocks, p.runs, p.slices, part, run_max, run_more, p.run_pitch)
 #define LRBI_PASS(P, WHOLE, COLUMN)                                                                                        \
     do {                                                                                                                   \
-        if (top > 0) LRBI_PASS_TOP(P, WHOLE, COLUMN, true);                                                                \
-        else LRBI_PASS_TOP(P, WHOLE, COLUMN, false);                                                                       \
+        if (top > 0) LRBI_PASS_TOP(P, WHOLE, COLUMN, true, false);                                                         \
+        else if (!COLUMN && past_cache) LRBI_PASS_TOP(P, WHOLE, COLUMN, false, !COLUMN);                                   \
+        else LRBI_PASS_TOP(P, WHOLE, COLUMN, false, false);                                                                \
     } while (0)
     const bool whole = N % p.shape.p == 0;
+    // Logits that do not fit the last-level cache, rows of whole lines (us, 65536 words, 4096 tokens bf16 107 -> 96; 71485 words, 1877 columns
+    // f32, whose rows share lines, with the gradient 403 -> 413; the gradient's loads that way: 300 -> 303)
+    const bool past_cache = V * N * (int64_t)sizeof(T) >= LRBI_STREAM_BYTES && (((uintptr_t)L | (uint64_t)(ldl * (int64_t)sizeof(T))) & 127) == 0;
     switch (p.shape.p) {
     case 1:
         if (column) LRBI_PASS(1, true, true);

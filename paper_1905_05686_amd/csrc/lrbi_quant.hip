@@ -24,7 +24,7 @@ typedef __bf16 q_bf16x8 __attribute__((ext_vector_type(8)));
 // with nothing, by the mask words' chain of loads (16000 x 9224 bf16 in 512 x 512 tiles 88 us = 4.2 TB/s, without a mask 73; 6000 x 3000 f16
 // in 300 x 300 tiles 17 and 11).  Loads return in order, so the mask's wait behind the weights'; asking for its first ones before the weights
 // cost more registers than it saved (16 on the small one, 89 on the large).
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void quant_pack_kernel(Geom g, const T *__restrict__ W, int64_t ldw, const uint32_t *__restrict__ Ip,
                                                          const uint32_t *__restrict__ Iz, unsigned char *__restrict__ codes, int64_t ldc,
                                                          unsigned char *__restrict__ scales, int64_t lds, int64_t segments)
@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void quant_pack_kernel(Geom g, const T *__rest
     const T *src = W + row * ldw + j0;
     StorePiece<T> p[PIECES];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) p[i] = store_load<T>(src + 512 * i, g.n - j0 - 512 * i);
+    for (int i = 0; i < PIECES; ++i) p[i] = store_load<STREAM>(src + 512 * i, g.n - j0 - 512 * i);
     uint32_t word = 0xFFFFFFFFu;
     if (Ip) {
         const int ti = (int)(row / g.r);
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void quant_pack_kernel(Geom g, const T *__rest
 }
 
 // A lane takes eight columns.  Bound by the values written (16000 x 9224 bf16 69 us = 5.4 TB/s, 6000 x 3000 f16 8.2).
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void quant_unpack_kernel(const unsigned char *__restrict__ codes, int64_t ldc,
                                                            const unsigned char *__restrict__ scales, int64_t lds, int64_t m, int64_t n,
                                                            T *__restrict__ W, int64_t ldw, int64_t pieces, bool is_short)
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void quant_unpack_kernel(const unsigned char *
     const int64_t at = wide_block() * 256 + threadIdx.x, row = store_row(at, pieces, is_short), p = at - row * pieces;
     if (row >= m) return;
     const uint32_t w = *reinterpret_cast<const uint32_t *>(codes + row * ldc + p * 4);
-    store_values<T>(W + row * ldw + p * 8, values4(T{}, w, scale_operand(scales[row * lds + (p >> 2)])), n - p * 8);
+    store_values<STREAM>(W + row * ldw + p * 8, values4(T{}, w, scale_operand(scales[row * lds + (p >> 2)])), n - p * 8);
 }
 
 // Y = Wq X.  The codes are read once, straight into registers, and that is what takes the time: 16384 x 16384 bf16, one column,
@@ -292,7 +292,9 @@ static int launch_pack_t(const Geom &g, const T *W, int64_t ldw, const uint32_t 
 {
     const int64_t segments = (g.n + 2047) / 2048, groups = (g.m + 3) / 4 * segments;
     if (groups > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    LRBI_LAUNCH(quant_pack_kernel<T>, wide_grid(groups, 256), dim3(256), 0, stream, g, W, ldw, Ip, Iz, codes, ldc, scales, lds, segments);
+    // (with the other direction, 16000 x 9224 bf16: 162 -> 128 us)
+    auto kern = g.m * g.n * (int64_t)sizeof(T) >= LRBI_STREAM_BYTES ? quant_pack_kernel<T, true> : quant_pack_kernel<T, false>;
+    LRBI_LAUNCH(kern, wide_grid(groups, 256), dim3(256), 0, stream, g, W, ldw, Ip, Iz, codes, ldc, scales, lds, segments);
     return LRBI_OK;
 }
 int launch_quant_pack(const Geom &g, lrbi_dtype dt, const void *dW, int64_t ldw, const uint32_t *dIp, const uint32_t *dIz, void *dCodes,
@@ -312,7 +314,8 @@ static int launch_unpack_t(const unsigned char *codes, int64_t ldc, const unsign
 {
     const int64_t pieces = (n + 7) / 8, groups = (m * pieces + 255) / 256;
     if (groups > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
-    LRBI_LAUNCH(quant_unpack_kernel<T>, wide_grid(groups, 256), dim3(256), 0, stream, codes, ldc, scales, lds, m, n, W, ldw, pieces,
+    auto kern = m * n * (int64_t)sizeof(T) >= LRBI_STREAM_BYTES ? quant_unpack_kernel<T, true> : quant_unpack_kernel<T, false>;
+    LRBI_LAUNCH(kern, wide_grid(groups, 256), dim3(256), 0, stream, codes, ldc, scales, lds, m, n, W, ldw, pieces,
                 groups * 256 < (int64_t)1 << 32);
     return LRBI_OK;
 }

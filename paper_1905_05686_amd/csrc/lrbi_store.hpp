@@ -61,13 +61,17 @@ template <typename T> struct StorePiece {
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) StoreUnaligned {
     uint32_t x, y, z, w;
 };
-// `left` values of the row from here on, zeros behind them
-template <typename T> __device__ __forceinline__ StorePiece<T> store_load(const T *src, int64_t left)
+// `left` values of the row from here on, zeros behind them.  STREAM: they are too many for the last-level cache.
+template <bool STREAM, typename T> __device__ __forceinline__ StorePiece<T> store_load(const T *src, int64_t left)
 {
     StorePiece<T> p;
     if (left >= 8) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            if constexpr (STREAM) {
+                p.v[i] = stream_load16(src + i * (16 / (int)sizeof(T)));
+                continue;
+            }
             const StoreUnaligned<T> u = reinterpret_cast<const StoreUnaligned<T> *>(src)[i];
             p.v[i] = make_uint4(u.x, u.y, u.z, u.w);
         }
@@ -79,11 +83,14 @@ template <typename T> __device__ __forceinline__ StorePiece<T> store_load(const 
     }
     return p;
 }
-template <typename T> __device__ __forceinline__ void store_values(T *dst, const StorePiece<T> &p, int64_t left)
+template <bool STREAM, typename T> __device__ __forceinline__ void store_values(T *dst, const StorePiece<T> &p, int64_t left)
 {
     if (left >= 8) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<StoreUnaligned<T> *>(dst)[i] = {p.v[i].x, p.v[i].y, p.v[i].z, p.v[i].w};
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            if constexpr (STREAM) stream_store16(dst + i * (16 / (int)sizeof(T)), p.v[i]);
+            else reinterpret_cast<StoreUnaligned<T> *>(dst)[i] = {p.v[i].x, p.v[i].y, p.v[i].z, p.v[i].w};
+        }
     } else {
         T e[8];
         __builtin_memcpy(e, &p, sizeof(e));
