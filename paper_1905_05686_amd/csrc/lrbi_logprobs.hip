@@ -19,8 +19,8 @@
 // found are ranked by counting.  (Reading every run that reaches the bound: 65536 words, 256 tokens, 20 top words 32 us
 // against 22.)
 //
-// Bounds.  65536 words, 4096 tokens bf16 (537 MB): the pass 122 to 128 us, reads at 4.3 TB/s; the finish 6; the gradient 187, read and
-// written at 5.7 TB/s.  With top words the pass is bound by its comparisons (about 14 vector instructions a logit: 256 tokens, 33.5 MB, 13
+// Bounds.  65536 words, 4096 tokens bf16 (537 MB): the pass 96 us, reads at 5.6 TB/s; the finish 6; the gradient 198 to 205, read and
+// written at 5.3 TB/s.  With top words the pass is bound by its comparisons (about 14 vector instructions a logit: 256 tokens, 33.5 MB, 13
 // us), the finish by one wavefront's chain of loads a column (9).
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>

@@ -21,9 +21,9 @@ typedef __bf16 q_bf16x8 __attribute__((ext_vector_type(8)));
 
 // A wavefront takes 2048 columns of a row: each lane forms one of their 64 mask words while the weights are on their way, then the
 // lanes go along them eight columns at a time, four lanes a block.  Bound by the weights read and, where tiles are small or line up
-// with nothing, by the mask words' chain of loads (16000 x 9224 bf16 in 512 x 512 tiles 88 us = 4.2 TB/s, without a mask 73; 6000 x 3000 f16
-// in 300 x 300 tiles 17 and 11).  Loads return in order, so the mask's wait behind the weights'; asking for its first ones before the weights
-// cost more registers than it saved (16 on the small one, 89 on the large).
+// with nothing, by the mask words' chain of loads (16000 x 9224 bf16 in 512 x 512 tiles 78 us = 4.8 TB/s; 6000 x 3000 f16 in 300 x 300
+// tiles 17, without a mask 11).  Loads return in order, so the mask's wait behind the weights'; asking for its first ones before the weights
+// cost more registers than it saved (1 us less on the small one, 1 more on the large).
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void quant_pack_kernel(Geom g, const T *__restrict__ W, int64_t ldw, const uint32_t *__restrict__ Ip,
                                                          const uint32_t *__restrict__ Iz, unsigned char *__restrict__ codes, int64_t ldc,
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void quant_pack_kernel(Geom g, const T *__rest
     }
 }
 
-// A lane takes eight columns.  Bound by the values written (16000 x 9224 bf16 69 us = 5.4 TB/s, 6000 x 3000 f16 8.2).
+// A lane takes eight columns.  Bound by the values written (16000 x 9224 bf16 51 us = 7.3 TB/s, 6000 x 3000 f16 8.2).
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void quant_unpack_kernel(const unsigned char *__restrict__ codes, int64_t ldc,
                                                            const unsigned char *__restrict__ scales, int64_t lds, int64_t m, int64_t n,
