@@ -586,9 +586,10 @@ def _store(device, pair, rows, cols, block_bytes):
     """Addresses and pitches of codes and scales that hold `rows` rows of `cols` values in blocks of 32."""
     codes, scales = pair
     blocks = -(-cols // 32)
-    if codes.dim() != 2 or scales.dim() != 2 or codes.element_size() != 1 or scales.element_size() != 1:
+    shape, scale_shape = codes.shape, scales.shape
+    if len(shape) != 2 or len(scale_shape) != 2 or codes.element_size() != 1 or scales.element_size() != 1:
         raise ValueError("codes and scales must be matrices of bytes")
-    (crows, ccols), (srows, scols) = codes.shape, scales.shape
+    (crows, ccols), (srows, scols) = shape, scale_shape
     if crows != rows or srows != rows:
         raise ValueError("codes and scales must have a row for each row")
     if ccols < block_bytes * blocks or scols < blocks:
@@ -613,34 +614,42 @@ def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
     """lrbi_quant_pack: W [m, n] with its pruned weights as zeros into 4-bit codes (uint8 [m, 16 per 32 columns]) and scale
     bytes (uint8 [m, 1 per 32 columns, rows of 4-byte pieces]).  Without factors nothing is pruned.  `out` = (codes, scales)
     reuses two tensors.  Returns (codes, scales)."""
-    if W.dim() != 2 or W.shape != (desc.m, desc.n) or (desc.n > 1 and W.stride(1) != 1):
+    m, n = desc.m, desc.n
+    if W.shape != (m, n):
+        raise ValueError("W must be a row-major [m, n] tensor")
+    ldw, inner = W.stride()
+    if n > 1 and inner != 1:
         raise ValueError("W must be a row-major [m, n] tensor")
     device = _device_of(W, "W")
     if out is None:
-        out = _new_store(desc.m, desc.n, 16, W.device)
-    cp, ldc, sp, lds = _store(device, out, desc.m, desc.n, 16)
+        out = _new_store(m, n, 16, W.device)
+    cp, ldc, sp, lds = _store(device, out, m, n, 16)
     _check(load_library().lrbi_quant_pack(
-        ctypes.byref(desc), _dtype_code(W), W.data_ptr(), W.stride(0), None if dIp is None else _ptr_on(device, dIp, "Ip"),
+        ctypes.byref(desc), _dtype_code(W), W.data_ptr(), ldw, None if dIp is None else _ptr_on(device, dIp, "Ip"),
         None if dIz is None else _ptr_on(device, dIz, "Iz"), cp, ldc, sp, lds, _stream_ptr(stream)), "lrbi_quant_pack")
     return out
 
 
 def _values_out(out, rows, cols, dtype, device):
+    """The values' tensor [rows, cols] (made here when there is none) and its leading dimension."""
     if out is None:
         import torch
-        return torch.empty((rows, cols), dtype=dtype, device=device)
-    if out.shape != (rows, cols) or out.dtype != dtype or (cols > 1 and out.stride(1) != 1):
+        return torch.empty((rows, cols), dtype=dtype, device=device), cols
+    if out.shape != (rows, cols) or out.dtype != dtype:
         raise ValueError("bad out tensor")
-    return out
+    ld, inner = out.stride()
+    if cols > 1 and inner != 1:
+        raise ValueError("bad out tensor")
+    return out, ld
 
 
 def quant_unpack(codes, scales, n: int, dtype, out=None, stream=None):
     """lrbi_quant_unpack: the values [m, n] of 4-bit codes, as numbers of `dtype`."""
     m = codes.shape[0]
     device = _device_of(codes, "codes")
-    out = _values_out(out, m, n, dtype, codes.device)
+    out, ldw = _values_out(out, m, n, dtype, codes.device)
     cp, ldc, sp, lds = _store(device, (codes, scales), m, n, 16)
-    _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _ptr_on(device, out, "W"), out.stride(0),
+    _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _ptr_on(device, out, "W"), ldw,
                                             _stream_ptr(stream)), "lrbi_quant_unpack")
     return out
 
@@ -667,14 +676,16 @@ def quant_matvec(codes, scales, X, out=None, stream=None):
 def checkpoint_pack(X, out=None, stream=None):
     """lrbi_checkpoint_pack: a layer input X [n, N] into 8-bit codes (uint8 [n, N rounded up to 32]) and scale bytes (uint8
     [n, 1 per 32 columns, rows of 4-byte pieces]).  `out` = (codes, scales) reuses two tensors.  Returns (codes, scales)."""
-    if X.dim() != 2 or (X.shape[1] > 1 and X.stride(1) != 1):
+    if X.dim() != 2:
         raise ValueError("X must be a row-major [n, N] tensor")
-    n, N = X.shape
+    (n, N), (ldx, inner) = X.shape, X.stride()
+    if N > 1 and inner != 1:
+        raise ValueError("X must be a row-major [n, N] tensor")
     device = _device_of(X, "X")
     if out is None:
         out = _new_store(n, N, 32, X.device)
     cp, ldc, sp, lds = _store(device, out, n, N, 32)
-    _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), X.data_ptr(), X.stride(0), n, N, cp, ldc, sp, lds,
+    _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), X.data_ptr(), ldx, n, N, cp, ldc, sp, lds,
                                                _stream_ptr(stream)), "lrbi_checkpoint_pack")
     return out
 
@@ -683,9 +694,9 @@ def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
     """lrbi_checkpoint_unpack: the values [n, N] of a checkpoint, as numbers of `dtype`."""
     n = codes.shape[0]
     device = _device_of(codes, "codes")
-    out = _values_out(out, n, N, dtype, codes.device)
+    out, ldx = _values_out(out, n, N, dtype, codes.device)
     cp, ldc, sp, lds = _store(device, (codes, scales), n, N, 32)
-    _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _ptr_on(device, out, "X"), out.stride(0),
+    _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _ptr_on(device, out, "X"), ldx,
                                                  _stream_ptr(stream)), "lrbi_checkpoint_unpack")
     return out
 
@@ -693,16 +704,18 @@ def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
 def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=None):
     """lrbi_checkpoint_grad: masked_grad with X given as a checkpoint: dW = (dY Xq^T) o decode(Ip, Iz), dY [m, N]."""
     m, n = desc.m, desc.n
-    if dY.dim() != 2 or dY.shape[0] != m:
+    if dY.dim() != 2:
+        raise ValueError("dY must be a row-major tensor")
+    (rows, N), (lddy, inner) = dY.shape, dY.stride()
+    if rows != m:
         raise ValueError("shape mismatch")
-    N = dY.shape[1]
-    if N > 1 and dY.stride(1) != 1:
+    if N > 1 and inner != 1:
         raise ValueError("dY must be a row-major tensor")
     device = _device_of(dY, "dY")
     cp, ldc, sp, lds = _store(device, (codes, scales), n, N, 32)
     out, lddw = _row_major_out(out, m, n, dY)
     _check(load_library().lrbi_checkpoint_grad(
-        ctypes.byref(desc), _dtype_code(dY), dY.data_ptr(), dY.stride(0), cp, ldc, sp, lds, N, _ptr_on(device, dIp, "Ip"),
+        ctypes.byref(desc), _dtype_code(dY), dY.data_ptr(), lddy, cp, ldc, sp, lds, N, _ptr_on(device, dIp, "Ip"),
         _ptr_on(device, dIz, "Iz"), _ptr_on(device, out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
     return out
 
