@@ -182,7 +182,7 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
                                                                      const unsigned char *__restrict__ XS, int64_t ldxs, int N,
                                                                      const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz,
                                                                      typename CgTypes<Tag>::elem *__restrict__ DW, int64_t lddw,
-                                                                     int64_t jblocks, int64_t blocks)
+                                                                     uint32_t jblocks, uint32_t blocks)
 {
     typedef typename CgTypes<Tag>::elem E;
     typedef typename CgTypes<Tag>::op Op;
@@ -202,8 +202,9 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
     uint4 areg[4][AV];
     uint4 xreg[2];
     uint32_t sreg[2];
-    auto load = [&](int64_t block, int slab) __attribute__((always_inline)) {
-        const int64_t ib = block / jblocks, i0 = ib * CG_B, j0 = (block - ib * jblocks) * CG_B;
+    auto load = [&](uint32_t block, int slab) __attribute__((always_inline)) {
+        const uint32_t ib = block / jblocks;
+        const int64_t i0 = (int64_t)ib * CG_B, j0 = (int64_t)(block - ib * jblocks) * CG_B;
         const int q = slab * CG_K + (tid & 7) * 8;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -250,14 +251,23 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
         }
     };
 
-    int64_t block = blockIdx.x;
+    // Workgroups go to the eight XCDs in turn: each XCD takes an eighth of the blocks, neighbouring ones, whose columns of dW share lines
+    // where rows are not made of whole ones, and whose workgroups share X.
+    uint32_t block = blockIdx.x, step = gridDim.x, end = blocks;
+    if (gridDim.x % 8 == 0) {
+        const uint32_t per = (blocks + 7) / 8;
+        step = gridDim.x / 8;
+        block = (blockIdx.x % 8) * per + blockIdx.x / 8;
+        end = (blockIdx.x % 8 + 1) * per < blocks ? (blockIdx.x % 8 + 1) * per : blocks;
+    }
+    if (block >= end) return; // the whole workgroup
     load(block, 0);
 #pragma unroll 1
-    for (; block < blocks; block += gridDim.x) {
-        const int64_t next = block + gridDim.x;
-        const int64_t ib = block / jblocks;
+    for (; block < end; block += step) {
+        const uint32_t next = block + step;
+        const uint32_t ib = block / jblocks;
         // this wavefront's 64 x 64
-        const int64_t i0 = ib * CG_B + wi * 64, j0 = (block - ib * jblocks) * CG_B + wj * 64;
+        const int64_t i0 = (int64_t)ib * CG_B + wi * 64, j0 = (int64_t)(block - ib * jblocks) * CG_B + wj * 64;
         CgMask q = cg_mask_begin(g, Ip, Iz, i0, j0, lined_up, lane);
         // ---- products
         f32x16 acc[2][2];
@@ -272,7 +282,7 @@ __global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_gr
             __syncthreads(); // the slab before has been read
             stage(s);
             const bool more = s + 1 < nslabs;
-            if (more || next < blocks) load(more ? block : next, more ? s + 1 : 0);
+            if (more || next < end) load(more ? block : next, more ? s + 1 : 0);
             __syncthreads();
             const unsigned char *as = smem + (wi * 64 + l32) * (CG_A_ROW * 2) + 16 * lg;
             const unsigned char *xs = smem + S::x_off + (wj * 64 + l32) * CG_X_ROW + 8 * lg;
@@ -583,6 +593,7 @@ static int launch_t(const Geom &g, const void *dDY, int64_t lddy, const void *dC
                     ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, ji);
         return LRBI_OK;
     }
+    if (blocks > 0x7FFFFFFF) return LRBI_ERR_SHAPE;
     const int64_t groups = blocks < at_once ? blocks : at_once;
     // dW past the last-level cache where it does not fit it and its rows are whole lines (16384 x 16384, batch 64 bf16 137 -> 111 us; rows
     // that begin inside a line, 4100 x 9224: 23 -> 42)
@@ -590,7 +601,7 @@ static int launch_t(const Geom &g, const void *dDY, int64_t lddy, const void *dC
     auto kern = stream_dw ? checkpoint_grad_kernel<Tag, true> : checkpoint_grad_kernel<Tag, false>;
     LRBI_SET_MAX_LDS(kern, SmemCg<Tag>::bytes);
     LRBI_LAUNCH(kern, dim3((unsigned)groups), dim3(CG_THREADS), SmemCg<Tag>::bytes, stream, g, (const E *)dDY, lddy, (const unsigned char *)dCodes,
-                ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, jblocks, blocks);
+                ldc, (const unsigned char *)dScales, lds, (int)N, dIp, dIz, (E *)dDW, lddw, (uint32_t)jblocks, (uint32_t)blocks);
     return LRBI_OK;
 }
 
