@@ -13,7 +13,7 @@
 //     store is two rows of 128 bytes (2324 x 4839, batch 211: 63 -> 40 us).
 //   * mask: tile sizes that are multiples of 64 and ranks up to 64: each wavefront fetches its block's slices of the factors before
 //     the products and forms its words behind them (Eq. 3); other shapes word by word.
-// 4100 x 9224, batch 131 f16 36 to 39 us (its 75 MB written alone 14), batch 40 23, batch 192 37: 16 and 7 more for each slab; 4096 x 4096,
+// 4100 x 9224, batch 131 f16 35 to 39 us (its 75 MB written alone 14), batch 40 23, batch 192 37: 16 and 7 more for each slab; 4096 x 4096,
 // batch 100 f32 29; 2000 x 8000 in 300 x 320 tiles, batch 777 f16 55.  With stores, loads or products left out (4096 x 9216, batch 128, 27 us)
 // 21, 23, 23: three workgroups a compute unit in turns of loading, multiplying and storing, no one of which is full.
 #include <type_traits>
