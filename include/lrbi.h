@@ -492,8 +492,8 @@ int lrbi_quant_matvec(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const v
  *   become NaN, alone.  Bytes past the last block of a row are left as they are.  One kernel launch.
  * lrbi_checkpoint_unpack: the values as numbers of `dtype`, exact for the type they came from.  One kernel launch.
  * lrbi_checkpoint_grad: lrbi_masked_grad with X the checkpoint's values: dW = (dY Xq^T) o I_a, the gradient with respect to
- *   W, read in 8 bits and widened exactly inside the kernel.  Arguments, masking, accumulation and rounding as there.  One
- *   kernel launch.
+ *   W, read in 8 bits and widened exactly inside the kernel.  Arguments, masking, accumulation and rounding as there.  N may
+ *   be less than what was packed: codes behind column N do not count.  One kernel launch.
  * Errors: those of the argument checks above; sizes not positive or beyond 2^31 - 256 are LRBI_ERR_SHAPE.
  */
 int lrbi_checkpoint_pack(lrbi_dtype dtype, const void *dX, int64_t ldx, int64_t n, int64_t N, void *dCodes, int64_t ldc,

@@ -3,8 +3,8 @@
 // the batch is what that product sums over, so a block's scale belongs to one step of its reduction.
 //
 // Both directions move each byte once and are bound by that (16384 x 4096 bf16: packing 45 us, taking out 31, 407 MB together at
-// 5.4 TB/s, above the 5.0 of a large copy; 800 x 100 f32 2.8 and 2.9 us).  Four lanes share a block, eight values (one or two 16-byte loads, eight bytes of codes)
-// each; the block's largest magnitude goes between them in two exchanges.
+// 5.4 TB/s, above the 5.0 of a large copy; 800 x 100 f32 3.0 us each).  Four lanes share a block, eight values (one or two
+// 16-byte loads, eight bytes of codes) each; the block's largest magnitude goes between them in two exchanges.
 #include "lrbi_internal.hpp"
 #include "lrbi_store.hpp"
 

@@ -177,12 +177,10 @@ __device__ __forceinline__ void cg_mask_end(CgMask &q, uint32_t *fz, bool lined_
 }
 
 template <typename Tag, bool STREAM>
-__global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_grad_kernel(Geom g, const typename CgTypes<Tag>::elem *__restrict__ DY, int64_t lddy,
-                                                                     const unsigned char *__restrict__ X, int64_t ldx,
-                                                                     const unsigned char *__restrict__ XS, int64_t ldxs, int N,
-                                                                     const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz,
-                                                                     typename CgTypes<Tag>::elem *__restrict__ DW, int64_t lddw,
-                                                                     uint32_t jblocks, uint32_t blocks)
+__global__ __launch_bounds__(CG_THREADS, CgTypes<Tag>::waves) void checkpoint_grad_kernel(
+    Geom g, const typename CgTypes<Tag>::elem *__restrict__ DY, int64_t lddy, const unsigned char *__restrict__ X, int64_t ldx,
+    const unsigned char *__restrict__ XS, int64_t ldxs, int N, const uint32_t *__restrict__ Ip, const uint32_t *__restrict__ Iz,
+    typename CgTypes<Tag>::elem *__restrict__ DW, int64_t lddw, uint32_t jblocks, uint32_t blocks)
 {
     typedef typename CgTypes<Tag>::elem E;
     typedef typename CgTypes<Tag>::op Op;

@@ -78,7 +78,8 @@ __global__ __launch_bounds__(256) void quant_unpack_kernel(const unsigned char *
 }
 
 // Y = Wq X.  The codes are read once, straight into registers, and that is what takes the time: 16384 x 16384 bf16, one column,
-// 142 MB in 29 us = 4.9 TB/s (8192 x 8192 11.5 us; 500 x 800 f32, latency alone, 5.2).  A wavefront owns 16 rows of W and takes 512 of their columns at a time, the next 512 under way while it multiplies:
+// 142 MB in 29 us = 4.9 TB/s (8192 x 8192 11.5 us; 500 x 800 f32, latency alone, 5.0).  A wavefront owns 16 rows of W and takes 512
+// of their columns at a time, the next 512 under way while it multiplies:
 // lane (row = lane % 16, block = lane / 16) loads the 16 bytes of one block of each 128 columns, and one piece of 16 scale
 // bytes for all of them.  The four products of 16 x 16 x 32 for 128 columns take eight codes of every block each (the order of
 // a sum's terms is free as long as both operands have the same one).  X goes through LDS as [eight rows][column], the eight
