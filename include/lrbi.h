@@ -463,7 +463,8 @@ int lrbi_nmf(const lrbi_desc *desc, lrbi_dtype dtype, const void *dW, int64_t ld
  * lrbi_quant_unpack: the values, as m x n numbers of `dtype`; exact at every scale that lrbi_quant_pack writes for this type,
  *   otherwise rounded to it.  One kernel launch.
  * lrbi_quant_matvec: Y = Wq X with the values Wq of codes and scales, X n x N and Y m x N row-major of `dtype` (ldx, ldy >= N;
- *   Y is overwritten).  f16 / bf16: products exact, fp32 sums; f32: X is taken as three bf16 parts whose products are exact.
+ *   Y is overwritten).  f16 / bf16: products exact, fp32 sums; f32: X is taken as three bf16 parts whose products are exact
+ *   (what of a number lies below 2^-133, the smallest bf16 number, is left out).
  *   The order of the sums is fixed (identical bits from call to call); one rounding to nearest-even on store.  Values that are
  *   no numbers of `dtype` (codes packed from another type) are rounded to it first.  X should be finite: an infinity times a
  *   zero code is NaN.  Any N; made for one to a few dozen columns (16, or 5 in f32, take the time of one).  For larger
@@ -493,7 +494,8 @@ int lrbi_quant_matvec(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const v
  * lrbi_checkpoint_unpack: the values as numbers of `dtype`, exact for the type they came from.  One kernel launch.
  * lrbi_checkpoint_grad: lrbi_masked_grad with X the checkpoint's values: dW = (dY Xq^T) o I_a, the gradient with respect to
  *   W, read in 8 bits and widened exactly inside the kernel.  Arguments, masking, accumulation and rounding as there.  N may
- *   be less than what was packed: codes behind column N do not count.  One kernel launch.
+ *   be less than what was packed: codes behind column N do not count.  f32: dY is taken as three
+ *   bf16 parts as lrbi_quant_matvec takes X.  One kernel launch.
  * Errors: those of the argument checks above; sizes not positive or beyond 2^31 - 256 are LRBI_ERR_SHAPE.
  */
 int lrbi_checkpoint_pack(lrbi_dtype dtype, const void *dX, int64_t ldx, int64_t n, int64_t N, void *dCodes, int64_t ldc,

@@ -162,6 +162,22 @@ def test_nan_codes_reach_their_weights():
         assert bad[:, 5].sum() == 31 and bad.sum() == 31 and not bad[3, 5] and (dW[3] == 0).all()
 
 
+def test_gradient_of_tiny_numbers():
+    """fp32 dY of 2^-100 to below the normal numbers: three bf16 parts hold each to 2^-133."""
+    print("checkpoint grad, tiny", flush=True)
+    m, n, N = 64, 96, 40
+    d = lrbi.Desc(m, n, 64, 96, 1)
+    ip, iz = device_factors(d, np.ones((1, m, 1), dtype=np.uint8), np.ones((1, 1, n), dtype=np.uint8))
+    gen = torch.Generator().manual_seed(5)
+    X = torch.randn(n, N, generator=gen).mul_(2.0 ** 60).to(dev())
+    dY = torch.ldexp(torch.randn(m, N, generator=gen), torch.arange(-140, -100).repeat_interleave(N * m // 40).reshape(m, N)).to(dev())
+    kept = lrbi.checkpoint_pack(X)
+    Xq = lrbi.checkpoint_unpack(*kept, N, torch.float32).double()
+    got, want, size = lrbi.checkpoint_grad(d, dY, *kept, ip, iz).double(), dY.double() @ Xq.T, dY.double().abs() @ Xq.abs().T
+    # parts: 2^-133 a product; sums: N roundings; the store: half a step
+    assert ((got - want).abs() <= 2.0 ** -133 * Xq.abs().sum(1)[None] + N * 2.0 ** -24 * size + 2.0 ** -24 * want.abs()).all()
+
+
 # large enough for 256 x 256 blocks; batches of few slabs of 32 columns, of eight and one more, of odd numbers of them
 @pytest.mark.parametrize("dtype,m,n,r,c,k,N", [("bf16", 4096, 4096, 512, 512, 32, 128), ("f16", 4096, 4096, 256, 256, 16, 288), ("bf16", 4096, 4096, 128, 64, 40, 544),
                                                ("f16", 2304, 4096, 256, 256, 16, 1024), ("bf16", 4096, 9216, 256, 256, 16, 96)])
