@@ -143,7 +143,8 @@ template <> struct StoreBits<__hip_bfloat16> {
 };
 
 // The codes of eight values at scale 2^e.  The conversion instructions scale and round (to nearest, ties to even) as the formats
-// ask, checked for every 16-bit number; 4 bits: what rounds past 6 is 6; 8 bits: what rounds past 448 and infinities are NaN.
+// ask (tested for every 16-bit number at every scale, fp32 numbers beside every tie, and back for every code at every scale byte);
+// 4 bits: what rounds past 6 is 6; 8 bits: what rounds past 448 and infinities are NaN.
 typedef __bf16 store_bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 store_f16x2 __attribute__((ext_vector_type(2)));
 typedef short store_s16x2 __attribute__((ext_vector_type(2)));
