@@ -493,8 +493,9 @@ int lrbi_quant_matvec(lrbi_dtype dtype, const void *dCodes, int64_t ldc, const v
  *   become NaN, alone.  Bytes past the last block of a row are left as they are.  One kernel launch.
  * lrbi_checkpoint_unpack: the values as numbers of `dtype`, exact for the type they came from.  One kernel launch.
  * lrbi_checkpoint_grad: lrbi_masked_grad with X the checkpoint's values: dW = (dY Xq^T) o I_a, the gradient with respect to
- *   W, read in 8 bits and widened exactly inside the kernel.  Arguments, masking, accumulation and rounding as there.  N may
- *   be less than what was packed: codes behind column N do not count.  f32: dY is taken as three
+ *   W, read in 8 bits and widened inside the kernel: exactly, if X was of the same type or dY is bf16 or f32; a checkpoint of
+ *   bf16 or f32 with f16 dY is rounded to f16 first, to an infinity beyond it.  Arguments, masking, accumulation and rounding
+ *   as there.  N may be less than what was packed: codes behind column N do not count.  f32: dY is taken as three
  *   bf16 parts as lrbi_quant_matvec takes X.  One kernel launch.
  * Errors: those of the argument checks above; sizes not positive or beyond 2^31 - 256 are LRBI_ERR_SHAPE.
  */

@@ -702,7 +702,8 @@ def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
 
 
 def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=None):
-    """lrbi_checkpoint_grad: masked_grad with X given as a checkpoint: dW = (dY Xq^T) o decode(Ip, Iz), dY [m, N]."""
+    """lrbi_checkpoint_grad: masked_grad with X given as a checkpoint: dW = (dY Xq^T) o decode(Ip, Iz), dY [m, N].  A bf16 or f32
+    checkpoint with f16 dY is rounded to f16, to infinities beyond its range."""
     m, n = desc.m, desc.n
     if dY.dim() != 2:
         raise ValueError("dY must be a row-major tensor")

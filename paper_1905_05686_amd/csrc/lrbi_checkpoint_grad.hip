@@ -6,7 +6,8 @@
 // written the first operands of the next one are on their way; its four wavefronts own 64 x 64 each, mask and write them on their own,
 // and wait for each other only when a slab of 64 batch columns changes hands.
 //   * dY: 16 bytes a load at any element's address, staged in LDS as [row][batch].
-//   * X: staged as codes, widened by the conversion instruction that also applies the scale, exactly, when they are read.
+//   * X: staged as codes, widened when they are read by the conversion instruction that also applies the scale: exactly, but for values of
+//     a wider type's checkpoint that are no f16 numbers (rounded; infinities beyond the type).
 //   * fp32 dY is split into three bf16 parts, y = y1 + y2 + y3 exactly (down to 2^-133); a checkpoint's values are bf16 numbers, so three 16-bit
 //     products, exact in fp32, do the work of sixteen times slower fp32 ones.
 //   * output: f16 / bf16 through LDS, eight rows of 128 bytes a store; fp32 with the roles of the two operands exchanged, so that a
