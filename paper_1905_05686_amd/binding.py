@@ -243,6 +243,21 @@ def _ptr_on(device, t, what):
     return t.data_ptr()
 
 
+def _empty(shape, dtype, device, stream, scratch=False):
+    """A new tensor for a call's kernels on `stream` (None: the current one).  It is that stream's memory: what the current stream
+    freed may still be read by kernels that it has queued.  `scratch` goes back to that stream when the call returns; what a
+    call hands out is marked as used by the current stream too, which goes on with it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if not scratch and stream != here:
+        t.record_stream(here)
+    return t
+
+
 def _scratch(workspace):
     """Address and size of an optional workspace."""
     if workspace is None:
@@ -294,11 +309,10 @@ def _product_operands(desc, W, X):
     return N, ldw, ldx
 
 
-def _row_major_out(out, rows, cols, like):
+def _row_major_out(out, rows, cols, like, stream=None):
     """The output tensor [rows, cols] (made here when there is none) and its leading dimension."""
     if out is None:
-        import torch
-        out = torch.empty((rows, cols), dtype=like.dtype, device=like.device)
+        out = _empty((rows, cols), like.dtype, like.device, stream)
     if out.shape != (rows, cols) or out.dtype != like.dtype:
         raise ValueError("bad out tensor")
     ld, inner = out.stride()
@@ -602,12 +616,12 @@ def _store(device, pair, rows, cols, block_bytes):
     return _ptr_on(device, codes, "codes"), ldc, _ptr_on(device, scales, "scales"), lds
 
 
-def _new_store(rows, cols, block_bytes, device):
+def _new_store(rows, cols, block_bytes, device, stream):
     """New codes and scales with the smallest pitches."""
     import torch
     blocks = -(-cols // 32)
-    return (torch.empty((rows, block_bytes * blocks), dtype=torch.uint8, device=device),
-            torch.empty((rows, -(-blocks // 4) * 4), dtype=torch.uint8, device=device))
+    return (_empty((rows, block_bytes * blocks), torch.uint8, device, stream),
+            _empty((rows, -(-blocks // 4) * 4), torch.uint8, device, stream))
 
 
 def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
@@ -622,7 +636,7 @@ def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
         raise ValueError("W must be a row-major [m, n] tensor")
     device = _device_of(W, "W")
     if out is None:
-        out = _new_store(m, n, 16, W.device)
+        out = _new_store(m, n, 16, W.device, stream)
     cp, ldc, sp, lds = _store(device, out, m, n, 16)
     _check(load_library().lrbi_quant_pack(
         ctypes.byref(desc), _dtype_code(W), W.data_ptr(), ldw, None if dIp is None else _ptr_on(device, dIp, "Ip"),
@@ -630,11 +644,10 @@ def quant_pack(desc: Desc, W, dIp=None, dIz=None, out=None, stream=None):
     return out
 
 
-def _values_out(out, rows, cols, dtype, device):
+def _values_out(out, rows, cols, dtype, device, stream):
     """The values' tensor [rows, cols] (made here when there is none) and its leading dimension."""
     if out is None:
-        import torch
-        return torch.empty((rows, cols), dtype=dtype, device=device), cols
+        return _empty((rows, cols), dtype, device, stream), cols
     if out.shape != (rows, cols) or out.dtype != dtype:
         raise ValueError("bad out tensor")
     ld, inner = out.stride()
@@ -647,7 +660,7 @@ def quant_unpack(codes, scales, n: int, dtype, out=None, stream=None):
     """lrbi_quant_unpack: the values [m, n] of 4-bit codes, as numbers of `dtype`."""
     m = codes.shape[0]
     device = _device_of(codes, "codes")
-    out, ldw = _values_out(out, m, n, dtype, codes.device)
+    out, ldw = _values_out(out, m, n, dtype, codes.device, stream)
     cp, ldc, sp, lds = _store(device, (codes, scales), m, n, 16)
     _check(load_library().lrbi_quant_unpack(_dtype_code(out), cp, ldc, sp, lds, m, n, _ptr_on(device, out, "W"), ldw,
                                             _stream_ptr(stream)), "lrbi_quant_unpack")
@@ -667,7 +680,7 @@ def quant_matvec(codes, scales, X, out=None, stream=None):
     cp, ldc, sp, lds = _store(device, (codes, scales), m, n, 16)
     if squeeze and out is not None:
         out = out.unsqueeze(1)
-    out, ldy = _row_major_out(out, m, N, X)
+    out, ldy = _row_major_out(out, m, N, X, stream)
     _check(load_library().lrbi_quant_matvec(_dtype_code(X), cp, ldc, sp, lds, m, n, X.data_ptr(), ldx, N, _ptr_on(device, out, "Y"), ldy,
                                             _stream_ptr(stream)), "lrbi_quant_matvec")
     return out[:, 0] if squeeze else out
@@ -683,7 +696,7 @@ def checkpoint_pack(X, out=None, stream=None):
         raise ValueError("X must be a row-major [n, N] tensor")
     device = _device_of(X, "X")
     if out is None:
-        out = _new_store(n, N, 32, X.device)
+        out = _new_store(n, N, 32, X.device, stream)
     cp, ldc, sp, lds = _store(device, out, n, N, 32)
     _check(load_library().lrbi_checkpoint_pack(_dtype_code(X), X.data_ptr(), ldx, n, N, cp, ldc, sp, lds,
                                                _stream_ptr(stream)), "lrbi_checkpoint_pack")
@@ -694,7 +707,7 @@ def checkpoint_unpack(codes, scales, N: int, dtype, out=None, stream=None):
     """lrbi_checkpoint_unpack: the values [n, N] of a checkpoint, as numbers of `dtype`."""
     n = codes.shape[0]
     device = _device_of(codes, "codes")
-    out, ldx = _values_out(out, n, N, dtype, codes.device)
+    out, ldx = _values_out(out, n, N, dtype, codes.device, stream)
     cp, ldc, sp, lds = _store(device, (codes, scales), n, N, 32)
     _check(load_library().lrbi_checkpoint_unpack(_dtype_code(out), cp, ldc, sp, lds, n, N, _ptr_on(device, out, "X"), ldx,
                                                  _stream_ptr(stream)), "lrbi_checkpoint_unpack")
@@ -714,7 +727,7 @@ def checkpoint_grad(desc: Desc, dY, codes, scales, dIp, dIz, out=None, stream=No
         raise ValueError("dY must be a row-major tensor")
     device = _device_of(dY, "dY")
     cp, ldc, sp, lds = _store(device, (codes, scales), n, N, 32)
-    out, lddw = _row_major_out(out, m, n, dY)
+    out, lddw = _row_major_out(out, m, n, dY, stream)
     _check(load_library().lrbi_checkpoint_grad(
         ctypes.byref(desc), _dtype_code(dY), dY.data_ptr(), lddy, cp, ldc, sp, lds, N, _ptr_on(device, dIp, "Ip"),
         _ptr_on(device, dIz, "Iz"), _ptr_on(device, out, "dW"), lddw, _stream_ptr(stream)), "lrbi_checkpoint_grad")
@@ -754,17 +767,14 @@ def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, 
     if out is None:
         if top < 0:
             raise ValueError("top must not be negative")
-        import torch
-        new = lambda *shape: torch.empty(shape, dtype=_f32, device=logits.device)  # noqa: E731
-        out = TokenLogprobs(None if tokens is None else new(N), new(N), new(2, N),
-                            torch.empty((top, N), dtype=_i64, device=logits.device), new(top, N))
+        new = lambda *shape, dtype=_f32: _empty(shape, dtype, logits.device, stream)  # noqa: E731
+        out = TokenLogprobs(None if tokens is None else new(N), new(N), new(2, N), new(top, N, dtype=_i64), new(top, N))
     logp, entropy, stats, top_ids, top_logp = out
     if (logp is None) != (tokens is None) or top_ids.shape != (top, N):
         raise ValueError("out is of a call with other results")
     if workspace is None:
         import torch
-        with torch.cuda.stream(stream):  # it belongs to the stream that uses it
-            workspace = torch.empty(token_logprobs_workspace_bytes(code, V, N, top), dtype=torch.uint8, device=logits.device)
+        workspace = _empty(token_logprobs_workspace_bytes(code, V, N, top), torch.uint8, logits.device, stream, scratch=True)
     row, tok_ptr, logp_ptr, ids_ptr, top_ptr = (N,), None, None, None, None
     if tokens is not None:
         tok_ptr, logp_ptr = _row_ptr(device, tokens, _i64, row, "tokens"), _row_ptr(device, logp, _f32, row, "out.logp")
@@ -788,7 +798,7 @@ def token_logprobs_grad(logits, tokens, result, g_logp=None, g_entropy=None, out
     if N > 1 and inner != 1:
         raise ValueError("logits must be a row-major [V, N] tensor")
     code, device = _dtype_code(logits), _device_of(logits, "logits")
-    out, lddl = _row_major_out(out, V, N, logits)
+    out, lddl = _row_major_out(out, V, N, logits, stream)
     row = (N,)
     _check(load_library().lrbi_token_logprobs_grad(
         code, logits.data_ptr(), ldl, V, N, None if tokens is None else _row_ptr(device, tokens, _i64, row, "tokens"),
