@@ -275,7 +275,7 @@ def decode_mask(desc: Desc, dIp, dIz, out=None, pitch_bytes=None, stream=None):
     if pitch_bytes is None:
         pitch_bytes = out.shape[1] if out is not None else default_pitch(desc.n)
     if out is None:
-        out = torch.empty((desc.m, pitch_bytes), dtype=torch.uint8, device=dIp.device)
+        out = _empty((desc.m, pitch_bytes), torch.uint8, dIp.device, stream)
     if out.dtype != torch.uint8 or not out.is_contiguous() or out.shape != (desc.m, pitch_bytes):
         raise ValueError("out must be a contiguous uint8 [m, pitch_bytes] tensor")
     _check(load_library().lrbi_decode_mask(ctypes.byref(desc), _dev_ptr(dIp, "Ip"), _dev_ptr(dIz, "Iz"),
@@ -309,7 +309,7 @@ def _product_operands(desc, W, X):
     return N, ldw, ldx
 
 
-def _row_major_out(out, rows, cols, like, stream=None):
+def _row_major_out(out, rows, cols, like, stream):
     """The output tensor [rows, cols] (made here when there is none) and its leading dimension."""
     if out is None:
         out = _empty((rows, cols), like.dtype, like.device, stream)
@@ -328,7 +328,7 @@ def masked_gemm(desc: Desc, W, dIp, dIz, X, out=None, workspace=None, stream=Non
     if squeeze:
         X = X.unsqueeze(1)
     N, ldw, ldx = _product_operands(desc, W, X)
-    out, ldy = _row_major_out(out, desc.m, N, W)
+    out, ldy = _row_major_out(out, desc.m, N, W, stream)
     ws_ptr, ws_bytes = _scratch(workspace)
     _check(load_library().lrbi_masked_gemm(
         ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), ldw, _dev_ptr(dIp, "Ip"), _dev_ptr(dIz, "Iz"),
@@ -340,12 +340,12 @@ def decode_and_gemm(desc: Desc, W, dIp, dIz, X, out=None, mask=None, pitch_bytes
     """lrbi_decode_and_gemm: the packed mask [m, pitch] (uint8) and Y = (W o mask) X from one call; arguments as
     for decode_mask and masked_gemm.  Returns (mask, Y)."""
     N, ldw, ldx = _product_operands(desc, W, X)
-    out, ldy = _row_major_out(out, desc.m, N, W)
+    out, ldy = _row_major_out(out, desc.m, N, W, stream)
     if pitch_bytes is None:
         pitch_bytes = mask.shape[1] if mask is not None else default_pitch(desc.n)
     import torch
     if mask is None:
-        mask = torch.empty((desc.m, pitch_bytes), dtype=torch.uint8, device=W.device)
+        mask = _empty((desc.m, pitch_bytes), torch.uint8, W.device, stream)
     if mask.dtype != torch.uint8 or not mask.is_contiguous() or mask.shape != (desc.m, pitch_bytes):
         raise ValueError("mask must be a contiguous uint8 [m, pitch_bytes] tensor")
     ws_ptr, ws_bytes = _scratch(workspace)
@@ -368,7 +368,6 @@ def masked_conv3x3(desc: Desc, W, dIp, dIz, act_padded, out=None, workspace=None
     """lrbi_masked_conv3x3: Y = (W o decode(Ip, Iz)) X for a 3 x 3, padding-1 convolution, X gathered from the
     activation.  W [m, 9 * cin] with column (kh * 3 + kw) * cin + ci; act_padded [batch, H + 2, Wd + 2, cin]
     contiguous with a zero border; returns Y [m, batch * H * Wd]."""
-    import torch
     if act_padded.dim() != 4 or not act_padded.is_contiguous() or act_padded.dtype != W.dtype:
         raise ValueError("act_padded must be a contiguous [batch, H + 2, Wd + 2, cin] tensor of W's dtype")
     batch, H, Wd, cin = act_padded.shape[0], act_padded.shape[1] - 2, act_padded.shape[2] - 2, act_padded.shape[3]
@@ -376,7 +375,7 @@ def masked_conv3x3(desc: Desc, W, dIp, dIz, act_padded, out=None, workspace=None
         raise ValueError("shape mismatch")
     N = batch * H * Wd
     if out is None:
-        out = torch.empty((desc.m, N), dtype=W.dtype, device=W.device)
+        out = _empty((desc.m, N), W.dtype, W.device, stream)
     if out.shape != (desc.m, N) or out.dtype != W.dtype or out.stride(1) != 1:
         raise ValueError("bad out tensor")
     ws_ptr, ws_bytes = _scratch(workspace)
@@ -434,12 +433,12 @@ def threshold_eval(desc: Desc, W, w_threshold: float, Mp, Mz, Tp, Tz, want_facto
         if kept.dtype != torch.int64 or cost.dtype != torch.float64 or kept.numel() != T or cost.numel() != T:
             raise ValueError("out must be (int64 [T], float64 [T])")
     else:
-        kept = torch.empty(T, dtype=torch.int64, device=W.device)
-        cost = torch.empty(T, dtype=torch.float64, device=W.device)
+        kept = _empty(T, torch.int64, W.device, stream)
+        cost = _empty(T, torch.float64, W.device, stream)
     ip = iz = None
     if want_factors:
-        ip = torch.empty((T * desc.r, (desc.k + 31) // 32), dtype=torch.int32, device=W.device)
-        iz = torch.empty((T * desc.k, 2 * ((desc.c + 63) // 64)), dtype=torch.int32, device=W.device)
+        ip = _empty((T * desc.r, (desc.k + 31) // 32), torch.int32, W.device, stream)
+        iz = _empty((T * desc.k, 2 * ((desc.c + 63) // 64)), torch.int32, W.device, stream)
     _check(load_library().lrbi_threshold_eval(
         ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), W.stride(0), float(w_threshold), int(method),
         float(amplify), _dev_ptr(Mp, "Mp"), _dev_ptr(Mz, "Mz"), _dev_ptr(Tp, "Tp"), _dev_ptr(Tz, "Tz"), _dev_ptr(ip, "Ip") if want_factors else None,
@@ -473,16 +472,16 @@ def search_thresholds(desc: Desc, W, w_threshold: float, Mp, Mz, target_sparsity
         if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
             raise ValueError("factor tensors must be contiguous float32 of shape %s" % (shape,))
     if workspace is None:
-        workspace = torch.empty(search_workspace_bytes(desc), dtype=torch.uint8, device=W.device)
+        workspace = _empty(search_workspace_bytes(desc), torch.uint8, W.device, stream, scratch=True)
     sp = (ctypes.c_double * len(sp_values))(*[float(v) for v in sp_values])
-    Tp = torch.empty(T, dtype=torch.float32, device=W.device)
-    Tz = torch.empty(T, dtype=torch.float32, device=W.device)
-    kept = torch.empty(T, dtype=torch.int64, device=W.device)
-    cost = torch.empty(T, dtype=torch.float64, device=W.device)
+    Tp = _empty(T, torch.float32, W.device, stream)
+    Tz = _empty(T, torch.float32, W.device, stream)
+    kept = _empty(T, torch.int64, W.device, stream)
+    cost = _empty(T, torch.float64, W.device, stream)
     ip = iz = None
     if want_factors:
-        ip = torch.empty((T * desc.r, (desc.k + 31) // 32), dtype=torch.int32, device=W.device)
-        iz = torch.empty((T * desc.k, 2 * ((desc.c + 63) // 64)), dtype=torch.int32, device=W.device)
+        ip = _empty((T * desc.r, (desc.k + 31) // 32), torch.int32, W.device, stream)
+        iz = _empty((T * desc.k, 2 * ((desc.c + 63) // 64)), torch.int32, W.device, stream)
     _check(load_library().lrbi_search_thresholds(
         ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), W.stride(0), float(w_threshold), int(method),
         float(amplify), _dev_ptr(Mp, "Mp"), _dev_ptr(Mz, "Mz"), float(target_sparsity), sp, len(sp_values), int(steps), int(tolerance), _dev_ptr(Tp, "Tp"),
@@ -509,7 +508,7 @@ def masked_gemm_t(desc: Desc, W, dIp, dIz, dY, out=None, workspace=None, stream=
     (ldw, w1), (lddy, y1) = W.stride(), dY.stride()
     if w1 != 1 or (N > 1 and y1 != 1) or W.dtype != dY.dtype:
         raise ValueError("W and dY must be row-major tensors of the same dtype")
-    out, lddx = _row_major_out(out, n, N, W)
+    out, lddx = _row_major_out(out, n, N, W, stream)
     ws_ptr, ws_bytes = _scratch(workspace)
     _check(load_library().lrbi_masked_gemm_t(
         ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), ldw, _dev_ptr(dIp, "Ip"), _dev_ptr(dIz, "Iz"),
@@ -528,7 +527,7 @@ def masked_grad(desc: Desc, dY, X, dIp, dIz, out=None, stream=None):
     (lddy, y1), (ldx, x1) = dY.stride(), X.stride()
     if (N > 1 and (y1 != 1 or x1 != 1)) or dY.dtype != X.dtype:
         raise ValueError("dY and X must be row-major tensors of the same dtype")
-    out, lddw = _row_major_out(out, m, n, dY)
+    out, lddw = _row_major_out(out, m, n, dY, stream)
     if out.stride(1) != 1:
         raise ValueError("bad out tensor")
     _check(load_library().lrbi_masked_grad(
@@ -560,7 +559,7 @@ def lstm_step(desc: Desc, W, dIp, dIz, XH, C, H1, H2=None, workspace=None, strea
     if W.stride(1) != 1 or (B > 1 and (XH.stride(1) != 1 or C.stride(1) != 1)) or XH.dtype != W.dtype:
         raise ValueError("row-major tensors of one dtype expected")
     if workspace is None:
-        workspace = torch.empty(lstm_step_workspace_bytes(desc, _dtype_code(W), B), dtype=torch.uint8, device=W.device)
+        workspace = _empty(lstm_step_workspace_bytes(desc, _dtype_code(W), B), torch.uint8, W.device, stream, scratch=True)
     _check(load_library().lrbi_lstm_step(
         ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), W.stride(0), _dev_ptr(dIp, "Ip"), _dev_ptr(dIz, "Iz"),
         _dev_ptr(XH, "XH"), XH.stride(0), B, _dev_ptr(C, "C"), C.stride(0), _dev_ptr(H1, "H1"), H1.stride(0),
@@ -588,7 +587,7 @@ def nmf(desc: Desc, W, Mp, Mz, iters: int, eps: float = 1e-9, method: int = 1, w
         if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
             raise ValueError("factor tensors must be contiguous float32 of shape %s" % (shape,))
     if workspace is None:
-        workspace = torch.empty(nmf_workspace_bytes(desc), dtype=torch.uint8, device=W.device)
+        workspace = _empty(nmf_workspace_bytes(desc), torch.uint8, W.device, stream, scratch=True)
     _check(load_library().lrbi_nmf(
         ctypes.byref(desc), _dtype_code(W), _dev_ptr(W, "W"), W.stride(0), int(method), float(w_threshold), float(amplify),
         _dev_ptr(Mp, "Mp"), _dev_ptr(Mz, "Mz"), int(iters), float(eps), _dev_ptr(workspace, "workspace"),

@@ -58,10 +58,23 @@ D = lrbi.Desc(64, 96, 32, 32, 4)
 W, X, DY = torch.zeros(64, 96), torch.zeros(96, 40), torch.zeros(64, 40)
 IP, IZ = torch.zeros(6 * 32, 1, dtype=torch.int32), torch.zeros(6 * 4, 2, dtype=torch.int32)
 CODES4, CODES8, SCALES = torch.zeros(64, 48, dtype=torch.uint8), torch.zeros(96, 64, dtype=torch.uint8), torch.zeros(96, 4, dtype=torch.uint8)
+MP, MZ, TP = torch.zeros(6, 32, 4), torch.zeros(6, 4, 32), torch.zeros(6)
+CONV, ACT = lrbi.Desc(64, 36, 32, 32, 4), torch.zeros(2, 5, 6, 4)
+CELL = lrbi.Desc(64, 48, 32, 32, 4)
 TOKENS, ROW = torch.zeros(40, dtype=torch.int64), torch.zeros(40)
 RESULT = lrbi.TokenLogprobs(ROW, ROW, torch.zeros(2, 40), None, None)
 # (call, tensors it hands out, scratch that it makes for itself)
 CALLS = {
+    "decode_mask": (lambda s: lrbi.decode_mask(D, IP, IZ, stream=s), 1, 0),
+    "masked_gemm": (lambda s: lrbi.masked_gemm(D, W, IP, IZ, X, stream=s), 1, 0),
+    "decode_and_gemm": (lambda s: lrbi.decode_and_gemm(D, W, IP, IZ, X, stream=s), 2, 0),
+    "masked_conv3x3": (lambda s: lrbi.masked_conv3x3(CONV, torch.zeros(64, 36), IP, IZ, ACT, stream=s), 1, 0),
+    "masked_gemm_t": (lambda s: lrbi.masked_gemm_t(D, W, IP, IZ, DY, stream=s), 1, 0),
+    "masked_grad": (lambda s: lrbi.masked_grad(D, DY, X, IP, IZ, stream=s), 1, 0),
+    "threshold_eval": (lambda s: lrbi.threshold_eval(D, W, 0.0, MP, MZ, TP, TP, want_factors=True, stream=s), 4, 0),
+    "search_thresholds": (lambda s: lrbi.search_thresholds(D, W, 0.0, MP, MZ, 0.9, [0.5], 4, 10, want_factors=True, stream=s), 6, 1),
+    "lstm_step": (lambda s: lrbi.lstm_step(CELL, torch.zeros(64, 48), IP, IZ, torch.zeros(48, 8), torch.zeros(16, 8), torch.zeros(16, 8), stream=s), 0, 1),
+    "nmf": (lambda s: lrbi.nmf(D, W, MP, MZ, 3, stream=s), 0, 1),
     "quant_pack": (lambda s: lrbi.quant_pack(D, W, IP, IZ, stream=s), 2, 0),
     "quant_unpack": (lambda s: lrbi.quant_unpack(CODES4, SCALES[:64], 96, torch.float32, stream=s), 1, 0),
     "quant_matvec": (lambda s: lrbi.quant_matvec(CODES4, SCALES[:64], X, stream=s), 1, 0),

@@ -21,7 +21,15 @@ def calls():
     codes4, codes8 = lrbi.quant_pack(d, W, ip, iz), lrbi.checkpoint_pack(X)
     tokens = torch.randint(0, M, (BATCH,), device=dev(), generator=gen)
     r, one = lrbi.token_logprobs(Y, tokens), torch.ones(BATCH, device=dev())
+    Mp, Mz = (torch.rand(shape, device=dev(), generator=gen) + 0.1 for shape in ((d.tiles, 128, 6), (d.tiles, 6, 64)))
+    search = lambda s: lrbi.search_thresholds(d, W, 0.1, Mp, Mz, 0.8, [0.5, 0.7], 4, 100, want_factors=True, stream=s)  # noqa: E731
     return {
+        "decode_mask": lambda s: (lrbi.decode_mask(d, ip, iz, stream=s),),
+        "masked_gemm": lambda s: (lrbi.masked_gemm(d, W, ip, iz, X, stream=s),),
+        "decode_and_gemm": lambda s: lrbi.decode_and_gemm(d, W, ip, iz, X, stream=s),
+        "masked_gemm_t": lambda s: (lrbi.masked_gemm_t(d, W, ip, iz, Y, stream=s),),
+        "masked_grad": lambda s: (lrbi.masked_grad(d, Y, X, ip, iz, stream=s),),
+        "search_thresholds": search,
         "quant_pack": lambda s: lrbi.quant_pack(d, W, ip, iz, stream=s),
         "quant_unpack": lambda s: (lrbi.quant_unpack(*codes4, N_IN, torch.float16, stream=s),),
         "quant_matvec": lambda s: (lrbi.quant_matvec(*codes4, X, stream=s),),
@@ -33,7 +41,8 @@ def calls():
     }
 
 
-@pytest.mark.parametrize("name", ["quant_pack", "quant_unpack", "quant_matvec", "checkpoint_pack", "checkpoint_unpack", "checkpoint_grad", "token_logprobs",
+@pytest.mark.parametrize("name", ["decode_mask", "masked_gemm", "decode_and_gemm", "masked_gemm_t", "masked_grad", "search_thresholds",
+                                  "quant_pack", "quant_unpack", "quant_matvec", "checkpoint_pack", "checkpoint_unpack", "checkpoint_grad", "token_logprobs",
                                   "token_logprobs_grad"])
 def test_call_on_another_stream(calls, name):
     print("streams", name, flush=True)
