@@ -610,8 +610,8 @@ def _store(device, pair, rows, cols, block_bytes):
     (ldc, c1), (lds, s1) = codes.stride(), scales.stride()
     if c1 != 1 or (s1 != 1 and scols > 1):
         raise ValueError("codes and scales must be row-major")
-    if rows == 1:  # a single row may have any stride: its pitch is what it holds
-        ldc, lds = ccols // 16 * 16, scols // 4 * 4
+    if rows == 1:  # a single row may have any stride, no pitch is added to it: its whole blocks, and the words that hold its scale bytes
+        ldc, lds = block_bytes * blocks, -(-blocks // 4) * 4
     return _ptr_on(device, codes, "codes"), ldc, _ptr_on(device, scales, "scales"), lds
 
 
