@@ -467,8 +467,9 @@ int lrbi_nmf(const lrbi_desc *desc, lrbi_dtype dtype, const void *dW, int64_t ld
  *   (what of a number lies below 2^-133, the smallest bf16 number, is left out).
  *   The order of the sums is fixed (identical bits from call to call); one rounding to nearest-even on store.  Values that are
  *   no numbers of `dtype` (codes packed from another type) are rounded to it first.  X should be finite: an infinity times a
- *   zero code is NaN.  Any N; made for one to a few dozen columns (16, or 5 in f32, take the time of one).  For larger
- *   batches lrbi_quant_unpack and lrbi_masked_gemm are the way.  One kernel launch.
+ *   zero code is NaN.  Any N; made for one to a few dozen columns: small layers take the time of one column for up to 8 (2000 x
+ *   4000 f16: 6.6 us, 16 columns 9, 32 13), large ones more with each (16384 x 16384 f16: 1 column 30 us, 2 36, 8 44, 16 55, 32 82;
+ *   f32: 1 36, 5 62, 10 94).  For larger batches lrbi_quant_unpack and lrbi_masked_gemm are the way.  One kernel launch.
  * Errors: those of the argument checks above; m, n, N not positive or beyond 2^31 - 256 are LRBI_ERR_SHAPE; one of the two
  * factors without the other LRBI_ERR_NULL.
  */

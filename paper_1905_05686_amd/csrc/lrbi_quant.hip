@@ -78,8 +78,9 @@ __global__ __launch_bounds__(256) void quant_unpack_kernel(const unsigned char *
 }
 
 // Y = Wq X.  The codes are read once, straight into registers, and that is what takes the time: 16384 x 16384 bf16, one column,
-// 142 MB in 29 us = 4.9 TB/s (8192 x 8192 11.5 us; 500 x 800 f32, latency alone, 5.0).  A wavefront owns 16 rows of W and takes 512
-// of their columns at a time, the next 512 under way while it multiplies:
+// 142 MB in 28.4 us = 5.0 TB/s (8192 x 8192 11.2 us; 500 x 800 f32, latency alone, 5.3).  More columns take longer: from 64 KB on X
+// comes in chunks, fetched and turned between two barriers by every workgroup (16384 x 16384 f16, 8 columns 39 us, 32 76; one f32 column, three
+// parts, 32).  A wavefront owns 16 rows of W and takes 512 of their columns at a time, the next 512 under way while it multiplies:
 // lane (row = lane % 16, block = lane / 16) loads the 16 bytes of one block of each 128 columns, and one piece of 16 scale
 // bytes for all of them.  The four products of 16 x 16 x 32 for 128 columns take eight codes of every block each (the order of
 // a sum's terms is free as long as both operands have the same one).  X goes through LDS as [eight rows][column], the eight
@@ -343,9 +344,11 @@ static int launch_matvec_t(const unsigned char *codes, int64_t ldc, const unsign
     const bool column = N == 1 && ldx == 1 && ((uintptr_t)X & 15) == 0;
     const bool fours = cols >= 4;
     // Wavefronts on different rows share X in LDS and add up fewer sums; there are fewer workgroups.  As many as leave one for
-    // every compute unit (us, with 1, 2, 4: 8192 x 8192, 7 columns f16 28 / 22 / 25; 16384 x 4096, 8 columns 20 / 14.5 / 12;
-    // 2000 x 4000, 3 columns 8.6 / 8.5 / 10), two for more than 8 operand columns, whose X fills LDS (6000 x 3000, 20 columns 13 / 10 /
-    // 12); one 16-bit column is little to share (300 x 16384 9.7 / 14 / 22, 16384 x 16384 34.8 / 38.6 / 34.5).
+    // every compute unit (us a call, with 1, 2, 4: 8192 x 8192, 7 columns f16 20.8 / 15.9 / 18.5, one column f32 13.3 / 14.6 / 14.5;
+    // 16384 x 4096, 8 columns f16 17.8 / 14.3 / 11.6; 16384 x 16384, one column f32 39.9 / 39.1 / 36.1; 2000 x 4000, 7 columns f16 6.5 / 7.5 /
+    // 9.2; 6000 x 3000, 7 columns f16 7.8 / 7.1 / 8.2, 2 columns f32 10.4 / 8.5 / 9.6), two for more than 8 operand columns, whose X fills LDS
+    // (with 2, 4: 6000 x 3000, 17 columns f16 12.4 / 15.1; 8192 x 8192, 16 columns 19.4 / 23.4; 16384 x 4096, 17 columns 29.3 / 21.3); one
+    // 16-bit column is little to share (300 x 16384 9.1 / 16.2 / 24.5, 16384 x 16384 30.2 / 40.8 / 32.7).
     int wr = m >= 64 * 256 ? 4 : m >= 32 * 256 || cols * PARTS > 8 ? 2 : 1;
     if (column && sizeof(T) == 2) wr = 1;
     const int64_t row_blocks = (m + 16 * wr - 1) / (16 * wr);
