@@ -607,6 +607,16 @@ static int launch_t(const Geom &g, const void *dDY, int64_t lddy, const void *dC
 int launch_checkpoint_grad(const Geom &g, lrbi_dtype dt, const void *dDY, int64_t lddy, const void *dCodes, int64_t ldc, const void *dScales,
                            int64_t lds, int64_t N, const uint32_t *dIp, const uint32_t *dIz, void *dDW, int64_t lddw, hipStream_t stream)
 {
+    // The 256 x 256 form by the rule of the gradient from 16-bit X (for 256 compute units).  Us here, 256 against 128, 256 x 256 tiles of
+    // rank 16:
+    //   * One round: 4096 x 4096 f16, batch 64 12.2 / 12.4, 128 13.8 / 14.3, 512 23.7 / 32.8, bf16, 256 21.0 / 19.8, 1024 40.2 / 54.9; 144
+    //     tiles, 2304 x 4096, bf16, 512 23.8 / 23.3, f16, 1024 28.9 / 38.7; 128 tiles, 2048 x 4096, bf16, 1024 32.6 / 31.4.
+    //   * Two: 8192 x 4096, f16, 512 44.5 / 59.3, bf16, 1024 77 / 105.  More: 8192 x 8192 in 512 x 512, rank 32, bf16, 256 79 / 71, 768 131 / 156,
+    //     f16, 512 90 / 118, 1024 142 / 206; 9216 x 9216, f16, 1024 196 / 267.
+    // Where that rule is off here: f16 gains earlier than it says (8192 x 4096, batch 256 31 / 35; 9216 x 9216, 512 130 / 149), so do long
+    // batches of half-full rounds (4096 x 9216, f16, 768 77 / 94, bf16, 1024 102 / 118; 2048 x 4096, f16, 2048 46 / 55), and tile widths of 64
+    // (2 j + 1) with more than 32 ranks lose in bf16 on short ones (8192 x 8192, rank 64, 128 69 / 54; 12288 x 4096, rank 40, 128 51 / 41; f16, 256
+    // 71 / 75).
     // (it addresses a block's rows of scales with 32-bit offsets too)
     if (dt != LRBI_F32 && grad256_wins(g, N) && grad256_ok(g, dDY, lddy, dCodes, ldc, N) && lds < (int64_t)1 << 22)
         return launch_grad256(g, dt, dDY, lddy, dCodes, ldc, dScales, lds, N, dIp, dIz, dDW, lddw, stream);
