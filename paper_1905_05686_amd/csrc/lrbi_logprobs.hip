@@ -16,12 +16,13 @@
 // the second largest.  A word that belongs to the top K lies in a run whose maximum is not below the K-th largest of any K or
 // more such maxima: the finishing wavefront takes the maxima of its 64 lanes' runs and, to 16 bits, their K-th largest as a bound.  The few
 // runs that reach it give their largest word; only those whose second largest reaches it too are read again.  The words
-// found are ranked by counting.  (Reading every run that reaches the bound: 65536 words, 256 tokens, 20 top words 32 us
-// against 22.)
+// found are ranked by counting.  (Reading every run that reaches the bound instead: 65536 words, 256 tokens, 20 top words 32 us
+// against 22 when the second largest was brought in.)
 //
 // Bounds.  65536 words, 4096 tokens bf16 (537 MB): the pass 96 us, reads at 5.6 TB/s; the finish 6; the gradient 198 to 205, read and
-// written at 5.3 TB/s.  With top words the pass is bound by its comparisons (about 14 vector instructions a logit: 256 tokens, 33.5 MB, 13
-// us), the finish by one wavefront's chain of loads a column (9).
+// written at 5.3 TB/s.  With top words the pass has 17.4 vector instructions a logit (counted; 8.0 without): 256 tokens, 33.5 MB, 13 to 14 us, of
+// which they are 7.4 at four clocks each, with the two halves of a run loaded one after the other; the finish is one wavefront's chain of
+// loads a column (9).
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
@@ -488,9 +489,9 @@ __device__ __forceinline__ void lp_write_top(const LpList<AHEAD> &l, int count, 
 }
 
 // Joins a column's slices and writes its results, one wavefront a column and workgroup: few columns go to as many compute units (four
-// wavefronts a workgroup: 94272 words, 66 tokens, 17 top words 21.9 us against 20.8, both kernels).
-// AHEAD: 0 without top words, otherwise as many as its runs fill in one round, up to 16 (us, 65536 words and below with 8, more
-// with 16 against 8: 94272 words, 66 tokens, 17 top words 21.2 -> 17.3; 131072 words, one token 14.4 -> 11.8).
+// wavefronts a workgroup, 8 ahead: 94272 words, 66 tokens, 17 top words 21.9 us against 20.8, both kernels).
+// AHEAD: 0 without top words, otherwise as many as its runs fill in one round, up to 16 (us a call with 8 and 16, both kernels: 94272
+// words, 66 tokens, 17 top words 21.2 / 18.9; 131072 words, 64 tokens, 20 top words 23.1 / 19.5, one token 14.6 / 12.2).
 template <typename T, int AHEAD>
 __global__ __launch_bounds__(64) void logprobs_finish_kernel(
     const T *__restrict__ L, int64_t ldl, int64_t V, int64_t N, const int64_t *__restrict__ tok, const float4 *__restrict__ part,
@@ -532,8 +533,8 @@ __global__ __launch_bounds__(64) void logprobs_finish_kernel(
 }
 
 // A single column without gaps, up to 32768 words, in one launch: a word of a served sequence.  1024 lanes take eight words at a
-// time, four lanes a run; the runs stay in LDS.  (10000 words f16, 8 top words: 9 us a call against 12 in two launches; 32768 words
-// bf16 10 against 12.4.)
+// time, four lanes a run; the runs stay in LDS.  (Us a call against two launches: 10000 words f16, 8 top words 8.7 / 11.7, the kernel 7.0;
+// 32768 words bf16, 20 top words 9.5 / 11.5, none 7.9 / 10.7.)
 static constexpr int LP_COLUMN_LANES = 1024;
 static constexpr int LP_COLUMN_SWEEPS = 4;
 static constexpr int LP_COLUMN_MOST = LP_COLUMN_LANES * 8 * LP_COLUMN_SWEEPS;
@@ -761,8 +762,8 @@ struct LpPlan {
 static LpPlan lp_plan(int es, int64_t V, int64_t N, int32_t top)
 {
     LpPlan p;
-    // The top words' comparisons are hidden by more wavefronts (65536 words, 256 tokens bf16: 8-byte pieces 24.6 us, 2-byte ones
-    // 22.5; 131072 words, 64 tokens 22.1 and 22.8).
+    // The top words' comparisons are hidden by more wavefronts (us a call, 8-byte pieces and 2-byte ones, bf16: 65536 words, 256 tokens
+    // 23.6 / 21.7, 11 tokens 13.4 / 13.0; 10000 words, 200 tokens 13.5 / 12.7; 131072 words, 64 tokens 19.0 / 19.5).
     p.shape = top > 0 ? lp_shape(es, V, N, 0, LP_RUN, 8, 1, 524288) : lp_shape(es, V, N, 0, LP_RUN, 8, 2, 131072);
     const int64_t all = (V + LP_RUN - 1) / LP_RUN;
     // runs a lane: as many as leave 2048 workgroups, eight for each compute unit
