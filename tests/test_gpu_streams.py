@@ -62,3 +62,27 @@ def test_call_on_another_stream(calls, name):
         got, want = (got[0], got[1][:, :3]), (want[0], want[1][:, :3])
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("name", ["quant_matvec", "checkpoint_grad", "token_logprobs", "masked_gemm", "search_thresholds"])
+def test_another_stream_in_a_graph(calls, name):
+    """Captured on a stream that forks from the captured one and joins it again; the first call's tensors are freed under capture."""
+    print("streams, graph", name, flush=True)
+    call, side = calls[name], torch.cuda.Stream()
+    want = call(None)
+    call(side)  # the kernels' first launch is outside the graph
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        call(side)
+        got = call(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for t in got:
+            t.view(torch.uint8).fill_(0x5A)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert all(torch.equal(a, b) for a, b in zip(call(None), want))  # the program's own work between the replays
