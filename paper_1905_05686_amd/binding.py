@@ -250,6 +250,8 @@ def _empty(shape, dtype, device, stream, scratch=False):
     import torch
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):  # anything with a stream's handle will do
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
     here = torch.cuda.current_stream(device)
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)

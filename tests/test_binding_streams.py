@@ -2,6 +2,7 @@
 stream still reads, and what is handed out is marked as used by the current stream.  Without a GPU: torch's allocation and streams are
 stood in for."""
 import contextlib
+import types
 
 import pytest
 import torch
@@ -11,7 +12,8 @@ from paper_1905_05686_amd import binding
 
 
 class _Stream:
-    cuda_stream = 5
+    def __init__(self, cuda_stream):
+        self.cuda_stream = cuda_stream
 
 
 class _Made(torch.Tensor):
@@ -28,7 +30,7 @@ class _Library:
 
 @pytest.fixture
 def torch_stand_in(monkeypatch):
-    here, side, made = _Stream(), _Stream(), []
+    here, side, made = _Stream(5), _Stream(6), []
     on = [here]
     empty = torch.empty
 
@@ -45,6 +47,8 @@ def torch_stand_in(monkeypatch):
         on.pop()
 
     monkeypatch.setattr(torch, "empty", make)
+    monkeypatch.setattr(torch.cuda, "Stream", _Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: {here.cuda_stream: here, side.cuda_stream: side}[handle])
     monkeypatch.setattr(torch.cuda, "stream", stream)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *device: on[-1])
     monkeypatch.setattr(binding, "load_library", lambda: _Library())
@@ -110,3 +114,11 @@ def test_current_stream(torch_stand_in, name):
             assert len(made) == outputs + scratch and all(t.owner is here and not t.marked for t in made)
     finally:
         binding._current_stream = old
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_stream_of_another_library(torch_stand_in, name):
+    """An object with nothing but a stream's handle."""
+    here, side, made = torch_stand_in
+    CALLS[name][0](types.SimpleNamespace(cuda_stream=side.cuda_stream))
+    assert all(t.owner is side for t in made) and sum(t.marked == [here] for t in made) == CALLS[name][1]

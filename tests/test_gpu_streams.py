@@ -1,5 +1,7 @@
 """Calls on another stream than the current one: the same bits as on it, and no tensor that they make lies where the current stream has just
 freed one, which its queued kernels may still read."""
+import types
+
 import numpy as np
 import pytest
 import torch
@@ -86,3 +88,16 @@ def test_another_stream_in_a_graph(calls, name):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         assert all(torch.equal(a, b) for a, b in zip(call(None), want))  # the program's own work between the replays
+
+
+@pytest.mark.parametrize("name", ["decode_mask", "quant_pack", "token_logprobs", "search_thresholds"])
+def test_a_streams_handle_alone(calls, name):
+    """Streams of other libraries: objects with a handle, the default stream's among them."""
+    print("streams, handles", name, flush=True)
+    call, side = calls[name], torch.cuda.Stream()
+    want = call(None)
+    torch.cuda.synchronize()
+    for handle in (side.cuda_stream, torch.cuda.default_stream().cuda_stream):
+        got = call(types.SimpleNamespace(cuda_stream=handle))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
